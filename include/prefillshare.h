@@ -351,6 +351,112 @@ int32_t ps_kv_stage_in(const ps_layout* layout, const void* dev_tables, const vo
 int32_t ps_layout_park(ps_pool* pool, ps_layout* layout);
 int32_t ps_layout_resume(ps_pool* pool, ps_layout* layout);
 
+/* ---- norm of queries and keys per head, rotation by position, cache write in one pass ------------------------------------
+ * What stands between a model's projections and a step's attention: every head row x[d] of q and k is normed,
+ * y = x * rsqrt(mean x^2 + eps) * weight, and the first rot_dim elements are turned pair by pair by an angle that is the
+ * token's position times the pair's rate, (a, b) -> (a cos - b sin, a sin + b cos); k then goes to the cache with v (Method Eq. 6,
+ * Background Eq. 4: a step's new entries join the cache that later queries attend to).  All of it in float32 and rounded
+ * once: to q_dtype, to the pool's format, or to e4m3 by the rules of ps_kv_append / ps_kv_ingest with float32 k in
+ * place of the source's.  head_dim 64, 128 or 256.
+ *
+ * turns: device uint64[rot_dim / 2], the rate of pair i as a fraction of a turn per position, times 2^64 (ps_rope_turns): a
+ * position's angle is then exact however far the position.  q_weight, k_weight: device [head_dim] in the rows' own type, 16-byte
+ * aligned; NULL: the rows are not normed.  rot_dim: even, 0 (no rotation; turns may be NULL) to head_dim; pairing: the elements
+ * (i, i + rot_dim / 2) (rot_dim a multiple of 16) or (2 i, 2 i + 1). */
+enum { PS_ROPE_HALVES = 0, PS_ROPE_NEIGHBOURS = 1 };
+typedef struct ps_rope {
+  const uint64_t* turns;
+  const void* q_weight;
+  const void* k_weight;
+  float eps; /* >= 0 */
+  int32_t rot_dim, pairing;
+} ps_rope;
+/* ps_rope_turns (host): out[i] = radians[i] / (2 pi) modulo 1, times 2^64; radians: angle per position, finite, >= 0. */
+int32_t ps_rope_turns(int32_t count, const double* radians, uint64_t* out);
+/* ps_rope_rows (device, asynchronous): the queries of any number of tokens (those of a partial prefill): src row t, head h at
+ * t * src_stride_row + h * src_stride_head (strides in elements, multiples of 16 bytes, pointers 16-byte aligned), q_dtype,
+ * num_q_heads heads; out [num_rows][Hq][d] contiguous, which may be src itself where that is contiguous; positions: device
+ * int32[num_rows].  Norm with q_weight. */
+int32_t ps_rope_rows(const ps_geometry* geometry, const ps_rope* rope, int64_t num_rows, const void* src, int64_t src_stride_row,
+                     int64_t src_stride_head, const int32_t* positions, void* out, void* stream);
+/* One row of q, k and v heads per request (element (r, h, c) at r * stride_row + h * stride_head + c; strides and pointers as
+ * above): views of one projection's output, say.  q: q_dtype; k, v: bf16 for bf16 and e4m3 pools, float32 for float32 pools.
+ * positions: device int32[R], of the token each request appends. */
+typedef struct ps_token_rows {
+  const void *q, *k, *v;
+  int64_t q_stride_row, q_stride_head, kv_stride_row, kv_stride_head; /* in elements */
+  const int32_t* positions;
+} ps_token_rows;
+/* ps_kv_append_rope (device, asynchronous): ps_kv_append of raw projections: the queries of every request, normed and rotated,
+ * to q_out [R][Hq][d] contiguous, and the new token of every request with one to append, k normed and rotated, to its place in
+ * the cache.  rows->q and q_out may be NULL together: the cache write alone.  dev_tables as for ps_kv_append. */
+int32_t ps_kv_append_rope(const ps_layout* layout, const void* dev_tables, const ps_rope* rope, const ps_token_rows* rows,
+                          void* q_out, void* kv_pool, float* kv_scales, void* stream);
+/* ps_kv_ingest_rope (device, asynchronous): ps_kv_ingest of raw projections (arguments as there); positions: device int32[T],
+ * one for every source token.  PS_ERR_UNSUPPORTED also for another head_dim than 64, 128, 256. */
+int32_t ps_kv_ingest_rope(const ps_layout* layout, const void* dev_tables, int32_t which, const ps_rope* rope, const void* src_k,
+                          const void* src_v, int64_t src_stride_tok, int64_t src_stride_head, const int32_t* positions,
+                          void* kv_pool, float* kv_scales, void* stream);
+
+/* ps_ingest_tokens (host): the tokens T that an ingest of one kind of segment takes and a gather gives, adopted blocks aside. */
+int32_t ps_ingest_tokens(const ps_layout* layout, int32_t which, int64_t* out);
+
+/* ---- reading a cache back -------------------------------------------------------------------------------------------
+ * ps_kv_gather (device, asynchronous): the stored segments of one kind (`which` as in ps_kv_ingest) into contiguous tensors,
+ * the hand-off of ps_kv_ingest the other way round (System Design, execution pipeline step 3): dst_k, dst_v as its sources, of
+ * dst_dtype PS_BF16 or PS_F32 whatever the pool holds; e4m3: code * scale of the tile in float32; rounded once to nearest even.
+ * Adopted blocks are left out, as an ingest leaves them out.  head_dim a multiple of 8. */
+int32_t ps_kv_gather(const ps_layout* layout, const void* dev_tables, int32_t which, const void* kv_pool, const float* kv_scales,
+                     int32_t dst_dtype, void* dst_k, void* dst_v, int64_t dst_stride_tok, int64_t dst_stride_head, void* stream);
+
+/* ---- a step over the blocks that matter to a query -----------------------------------------------------------------------
+ * A decode step reads its whole cache (Background Eq. 4).  Where a shared context is long, a request may attend to a bounded
+ * number of its blocks instead, chosen anew at every step by a cheap score, and to all of its private tokens:
+ *   ps_block_summaries  once a context is stored: eight bits a channel of every block's largest and smallest key;
+ *   ps_layout_select    a *selection*: a layout of its own over the base layout's batch whose block lists, one per request and KV
+ *                       head, hold the chosen blocks; planned, uploaded and released like any other;
+ *   ps_select_blocks    per step (and layer): scores, and the lists written into the selection's uploaded tables;
+ *   ps_decode_attention (or its parts, with or without a workspace) on the selection: the step.
+ *
+ * ps_block_summaries (device, asynchronous): for every block of the segments of one kind (`which` as in ps_kv_ingest; adopted
+ * blocks have theirs from the layout they were adopted from): summaries int8 [num_blocks][Hkv][2][d] (largest, smallest key of
+ * every channel over the block's stored tokens), summary_scales float32 [num_blocks][Hkv], num_blocks those of the pool.  With
+ * a the largest magnitude of both, scale = a * (the float32 nearest to 1/127) in float32 (1 where that is below the smallest
+ * normal number), code = round to nearest even of x / scale, at most 127.  A key that is not a number is passed over (0 where a channel has no other), an infinite one
+ * counts as the largest finite number.  summaries 16-byte aligned.  head_dim 64, 128 or 256. */
+int32_t ps_block_summaries(const ps_layout* layout, const void* dev_tables, int32_t which, const void* kv_pool,
+                           const float* kv_scales, int8_t* summaries, float* summary_scales, void* stream);
+/* blocks: how many blocks of its shared context (root, then the visible part of the prefix) a request attends to per KV head;
+ * a shorter context is attended to whole.  Always among them: the first keep_first (>= 0) and the last keep_last (>= 1) of the
+ * context, and a root's partly filled last block.  blocks >= keep_first + keep_last, one more for a layout with roots. */
+typedef struct ps_select_options {
+  int32_t blocks, keep_first, keep_last;
+} ps_select_options;
+/* ps_layout_select (host): a selection over `base` as it is now, with default plan options.  It holds no references: the caller
+ * releases it (ps_layout_release with any pool) no later than the blocks of base are to be used otherwise.  Until the first
+ * ps_select_blocks its lists name the beginning of every context (and its last block).  Its own calls are upload, replan, the
+ * attention passes and the merge, and the views; what changes or stores a batch (append, ingest, park, set_visible, ...) is refused
+ * with PS_ERR_INVALID_ARG.  PS_ERR_UNSUPPORTED: more than 64 query heads per KV head, contexts of more than 65536 blocks, another
+ * head_dim than 64, 128, 256.
+ * ps_layout_select_follow (host): brings a selection in line with its base after ps_layout_append, ps_layout_set_visible or
+ * ps_layout_replan there; upload it again afterwards.  An append that leaves the plan's structure alone is patched in, as there. */
+int32_t ps_layout_select(const ps_layout* base, const ps_select_options* options, ps_layout** out);
+int32_t ps_layout_select_follow(const ps_layout* base, ps_layout* selection);
+/* Where the lists lie in the selection's uploaded tables (host views, valid until the next follow/release): request r's list for
+ * KV head h is the int32 words [h * head_stride + list_indptr[r], h * head_stride + list_indptr[r + 1]): physical block ids in the
+ * order of the context, a root's partly filled last block aside.  list_indptr is int32[R + 1]. */
+int32_t ps_select_lists(const ps_layout* selection, const int32_t** list_indptr, int64_t* head_stride);
+/* Scratch memory of ps_select_blocks, 16-byte aligned; nothing in it needs clearing. */
+int64_t ps_select_workspace_bytes(const ps_layout* selection);
+/* ps_select_blocks (device, asynchronous): q [R][Hq][d] as for the attention.  A query row's codes are round to nearest even of
+ * q / s_q with s_q from max |q| as for the summaries (what is not a number counts as 0).  The score of a block for a request and
+ * KV head is the largest over the group's query heads of (float(sum over c of max(q_c, 0) hi_c + min(q_c, 0) lo_c) * s_block) * s_q:
+ * a whole number under 2^24 and two float32 products, so a choice is the same bits wherever it is made.  The highest scores are
+ * taken, the lower position first where they are equal.  base_tables, selection_tables: current uploads of both; base must be what
+ * the selection last followed (PS_ERR_INVALID_ARG). */
+int32_t ps_select_blocks(const ps_layout* base, const void* base_tables, const ps_layout* selection, void* selection_tables,
+                         const void* q, const int8_t* summaries, const float* summary_scales, void* workspace, void* stream);
+
 const char* ps_strerror(int32_t status);
 int32_t ps_last_hip_error(void);
 

@@ -18,6 +18,9 @@ two-level oracle on the flattened batch.  Adoption of a cached context's blocks 
 tests/test_oracle_layout.py) is pinned by a hand-worked instance, its rules, and attention over the
 continued context against the unpaged definition.  Staging of cold blocks (staging.py; tests/test_oracle_staging.py)
 is pinned by a hand-worked park / resume sequence, the block-count identity, and the requirement that
-a parked, overwritten and resumed batch reads back bit for bit.  No function here is unpinned.
+a parked, overwritten and resumed batch reads back bit for bit.  Norm and rotation (rope.py; tests/test_oracle_rope.py) are pinned by
+complex arithmetic, the invariance of products under a common shift, and norms; block summaries and selection (select.py;
+tests/test_oracle_select.py) by brute force in Python integers, the bound that a summary is, and attention over a selection of
+everything.  No function here is unpinned.
 """
-from . import attention, fp8, kv_update, layout, staging  # noqa: F401
+from . import attention, fp8, kv_update, layout, rope, select, staging  # noqa: F401

@@ -17,6 +17,8 @@ PS_STATIC_WORKSPACE_BYTES = 64 << 20
 PS_F32, PS_BF16, PS_FP8_E4M3 = 0, 1, 2
 PS_VARIANT_AUTO, PS_VARIANT_WAVE, PS_VARIANT_MFMA = 0, 1, 2
 PS_KV_POLICY_AUTO, PS_KV_POLICY_STREAM, PS_KV_POLICY_CACHEABLE = 0, 1, 2
+PS_ROPE_HALVES, PS_ROPE_NEIGHBOURS = 0, 1
+PAIRING = {"halves": PS_ROPE_HALVES, "neighbours": PS_ROPE_NEIGHBOURS}
 DTYPE_CODE = {"f32": PS_F32, "bf16": PS_BF16, "fp8_e4m3": PS_FP8_E4M3}
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libprefillshare.so")
@@ -31,6 +33,8 @@ EXPORTS = [
     "ps_layout_set_visible", "ps_layout_request_list", "ps_kv_layout_tree", "ps_layout_root_tables",
     "ps_kv_layout_adopt", "ps_blocks_needed", "ps_layout_state", "ps_stage_layout", "ps_kv_stage_out", "ps_kv_stage_in", "ps_layout_park",
     "ps_layout_resume", "ps_probe_read", "ps_decode_attention_static",
+    "ps_rope_turns", "ps_rope_rows", "ps_kv_append_rope", "ps_kv_ingest_rope", "ps_kv_gather", "ps_block_summaries",
+    "ps_ingest_tokens", "ps_layout_select", "ps_layout_select_follow", "ps_select_lists", "ps_select_workspace_bytes", "ps_select_blocks",
     "ps_strerror", "ps_last_hip_error",
 ]
 
@@ -39,7 +43,7 @@ EXPORTS = [
 DEVICE_EXPORTS = {
     "ps_layout_upload", "ps_layout_upload_wait", "ps_prefix_attention", "ps_suffix_attention", "ps_prefix_suffix_attention", "ps_merge_states",
     "ps_decode_attention", "ps_decode_attention_static", "ps_kv_append", "ps_layout_upload_append", "ps_kv_ingest", "ps_kv_stage_out", "ps_kv_stage_in",
-    "ps_probe_read",
+    "ps_probe_read", "ps_rope_rows", "ps_kv_append_rope", "ps_kv_ingest_rope", "ps_kv_gather", "ps_block_summaries", "ps_select_blocks",
     "ps_last_hip_error",
 }
 # Test hook: path of a build of the host side alone (block pool, tables, split plan) under AddressSanitizer / UBSan
@@ -70,6 +74,20 @@ class ps_plan_options(C.Structure):
                 ("kv_cache_policy", C.c_int32)]
 
 
+class ps_rope(C.Structure):
+    _fields_ = [("turns", C.c_size_t), ("q_weight", C.c_size_t), ("k_weight", C.c_size_t), ("eps", C.c_float),
+                ("rot_dim", C.c_int32), ("pairing", C.c_int32)]
+
+
+class ps_token_rows(C.Structure):
+    _fields_ = [("q", C.c_size_t), ("k", C.c_size_t), ("v", C.c_size_t), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64),
+                ("kv_stride_row", C.c_int64), ("kv_stride_head", C.c_int64), ("positions", C.c_size_t)]
+
+
+class ps_select_options(C.Structure):
+    _fields_ = [("blocks", C.c_int32), ("keep_first", C.c_int32), ("keep_last", C.c_int32)]
+
+
 _LIB = None
 _I32P = C.POINTER(C.c_int32)
 
@@ -91,6 +109,7 @@ def _lib():
         lib.ps_strerror.argtypes = [C.c_int32]
         lib.ps_layout_device_bytes.restype = C.c_int64
         lib.ps_workspace_bytes.restype = C.c_int64
+        lib.ps_select_workspace_bytes.restype = C.c_int64
         # the calls of a serving loop take plain addresses: declared once, ctypes converts them without an object each (as
         # integers, since a declared pointer would take text and ctypes objects too)
         if not host_only:
@@ -98,6 +117,8 @@ def _lib():
                                 "ps_prefix_suffix_attention": 7, "ps_merge_states": 6, "ps_decode_attention": 9,
                                 "ps_decode_attention_static": 8, "ps_kv_append": 7, "ps_layout_upload_append": 7}.items():
                 getattr(lib, name).argtypes = [C.c_void_p] + [C.c_size_t] * (count - 1)
+            lib.ps_kv_append_rope.argtypes = [C.c_void_p, C.c_size_t, C.POINTER(ps_rope), C.POINTER(ps_token_rows)] + [C.c_size_t] * 4
+            lib.ps_select_blocks.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p] + [C.c_size_t] * 6
         for name in EXPORTS:
             if not (host_only and name in DEVICE_EXPORTS):
                 getattr(lib, name)                  # fail early if a symbol is missing
@@ -431,6 +452,82 @@ def ps_kv_stage_in(layout, dev_tables, image, kv_pool, kv_scales, stream=0):
 def ps_probe_read(dev_buf, nbytes: int, pattern: int, num_workgroups: int, stream=0):
     _check(_lib().ps_probe_read(_p(dev_buf), C.c_int64(nbytes), C.c_int32(pattern), C.c_int32(num_workgroups),
                                 _p(stream)), "ps_probe_read")
+
+
+# ---- norm, rotation and cache write in one pass; reading back ----------------------------------------
+def ps_rope_turns(radians) -> np.ndarray:
+    """Rates as 64-bit fractions of a turn per position."""
+    rad = np.ascontiguousarray(radians, dtype=np.float64)
+    out = np.zeros(rad.size, np.uint64)
+    _check(_lib().ps_rope_turns(C.c_int32(rad.size), rad.ctypes.data_as(C.POINTER(C.c_double)),
+                                out.ctypes.data_as(C.POINTER(C.c_uint64))), "ps_rope_turns")
+    return out
+
+
+def ps_rope_rows(geo: ps_geometry, rope: ps_rope, num_rows: int, src, src_stride_row: int, src_stride_head: int, positions, out, stream=0):
+    _check(_lib().ps_rope_rows(C.byref(geo), C.byref(rope), C.c_int64(num_rows), _p(src), C.c_int64(src_stride_row),
+                               C.c_int64(src_stride_head), _p(positions), _p(out), _p(stream)), "ps_rope_rows")
+
+
+def ps_kv_append_rope(layout, dev_tables, rope: ps_rope, rows: ps_token_rows, q_out, kv_pool, kv_scales, stream=0):
+    status = _lib().ps_kv_append_rope(layout, int(dev_tables or 0), rope, rows, int(q_out or 0), int(kv_pool or 0), int(kv_scales or 0),
+                                      int(stream or 0))
+    if status != PS_OK:
+        raise PsError(status, "ps_kv_append_rope")
+
+
+def ps_kv_ingest_rope(layout, dev_tables, which: int, rope: ps_rope, src_k, src_v, src_stride_tok: int, src_stride_head: int, positions,
+                      kv_pool, kv_scales, stream=0):
+    _check(_lib().ps_kv_ingest_rope(layout, _p(dev_tables), C.c_int32(which), C.byref(rope), _p(src_k), _p(src_v),
+                                    C.c_int64(src_stride_tok), C.c_int64(src_stride_head), _p(positions), _p(kv_pool), _p(kv_scales),
+                                    _p(stream)), "ps_kv_ingest_rope")
+
+
+def ps_kv_gather(layout, dev_tables, which: int, kv_pool, kv_scales, dst_dtype: int, dst_k, dst_v, dst_stride_tok: int,
+                 dst_stride_head: int, stream=0):
+    _check(_lib().ps_kv_gather(layout, _p(dev_tables), C.c_int32(which), _p(kv_pool), _p(kv_scales), C.c_int32(dst_dtype), _p(dst_k),
+                               _p(dst_v), C.c_int64(dst_stride_tok), C.c_int64(dst_stride_head), _p(stream)), "ps_kv_gather")
+
+
+def ps_ingest_tokens(layout, which: int) -> int:
+    out = C.c_int64()
+    _check(_lib().ps_ingest_tokens(layout, C.c_int32(which), C.byref(out)), "ps_ingest_tokens")
+    return out.value
+
+
+# ---- a step over chosen blocks -------------------------------------------------------------------------
+def ps_block_summaries(layout, dev_tables, which: int, kv_pool, kv_scales, summaries, summary_scales, stream=0):
+    _check(_lib().ps_block_summaries(layout, _p(dev_tables), C.c_int32(which), _p(kv_pool), _p(kv_scales), _p(summaries),
+                                     _p(summary_scales), _p(stream)), "ps_block_summaries")
+
+
+def ps_layout_select(layout, blocks: int, keep_first: int = 1, keep_last: int = 2):
+    out = C.c_void_p()
+    opt = ps_select_options(blocks, keep_first, keep_last)
+    _check(_lib().ps_layout_select(layout, C.byref(opt), C.byref(out)), "ps_layout_select")
+    return out
+
+
+def ps_layout_select_follow(layout, selection):
+    _check(_lib().ps_layout_select_follow(layout, selection), "ps_layout_select_follow")
+
+
+def ps_select_lists(selection, num_requests: int):
+    """(list_indptr[R + 1], head_stride): where the block lists lie in the selection's tables, in int32 words."""
+    ip, stride = _I32P(), C.c_int64()
+    _check(_lib().ps_select_lists(selection, C.byref(ip), C.byref(stride)), "ps_select_lists")
+    return _view(ip, num_requests + 1), stride.value
+
+
+def ps_select_workspace_bytes(selection) -> int:
+    return int(_lib().ps_select_workspace_bytes(selection))
+
+
+def ps_select_blocks(layout, dev_tables, selection, selection_tables, q, summaries, summary_scales, workspace, stream=0):
+    status = _lib().ps_select_blocks(layout, int(dev_tables or 0), selection, int(selection_tables or 0), int(q or 0), int(summaries or 0),
+                                     int(summary_scales or 0), int(workspace or 0), int(stream or 0))
+    if status != PS_OK:
+        raise PsError(status, "ps_select_blocks")
 
 
 def ps_layout_park(pool, layout):

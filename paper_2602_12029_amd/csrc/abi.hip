@@ -262,6 +262,7 @@ int32_t ps_layout_upload(const ps_layout* lay, void* dev_tables, void* stream) {
 int32_t ps_layout_upload_append(const ps_layout* lay, void* dev_tables, const void* new_k, const void* new_v, void* kv_pool,
                                 float* kv_scales, void* stream) {
   StepTokens tokens{new_k, new_v, kv_pool, kv_scales, false};
+  if (lay && lay->sel) return PS_ERR_INVALID_ARG;
   const bool can_store = lay && !lay->parked && lay->num_requests > 0 && new_k && new_v && kv_pool &&
                          (lay->geo.kv_dtype != PS_FP8_E4M3 || kv_scales);
   if (int32_t rc = upload_tables(lay, dev_tables, stream, can_store ? &tokens : nullptr)) return rc;
@@ -311,7 +312,7 @@ int32_t ps_prefix_suffix_attention(const ps_layout* lay, const void* dev_tables,
 
 int32_t ps_kv_ingest(const ps_layout* lay, const void* dev_tables, int32_t which, const void* src_k, const void* src_v,
                      int64_t src_stride_tok, int64_t src_stride_head, void* kv_pool, float* kv_scales, void* stream) {
-  if (!lay || !dev_tables || which < 0 || which > 2 || lay->parked) return PS_ERR_INVALID_ARG;
+  if (!lay || !dev_tables || which < 0 || which > 2 || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
   const ps_geometry& g = lay->geo;
   const size_t entries = which == 0 ? lay->prefix_blk.size() : (which == 1 ? lay->suffix_blk.size() : lay->root_blk.size());
   if (entries == 0) return PS_OK;
@@ -328,7 +329,7 @@ int32_t ps_kv_ingest(const ps_layout* lay, const void* dev_tables, int32_t which
 
 int32_t ps_kv_append(const ps_layout* lay, const void* dev_tables, const void* new_k, const void* new_v, void* kv_pool,
                      float* kv_scales, void* stream) {
-  if (!lay || !dev_tables || lay->parked) return PS_ERR_INVALID_ARG;
+  if (!lay || !dev_tables || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
   if (lay->num_requests == 0) return PS_OK;
   if (!new_k || !new_v || !kv_pool || (lay->geo.kv_dtype == PS_FP8_E4M3 && !kv_scales)) return PS_ERR_INVALID_ARG;
   if (int32_t rc = psdev::launch_kv_append(lay, dev_tables, new_k, new_v, kv_pool, kv_scales,
@@ -341,7 +342,7 @@ namespace {
 
 int32_t stage(const ps_layout* lay, const void* dev_tables, bool to_image, void* kv_pool, float* kv_scales, void* image,
               void* stream) {
-  if (!lay || !dev_tables || lay->parked) return PS_ERR_INVALID_ARG;
+  if (!lay || !dev_tables || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
   int64_t scales_off = 0, total = 0;
   ps_stage_layout(lay, nullptr, &scales_off, &total);
   if (lay->prefix_blk.empty() && lay->suffix_blk.empty() && lay->root_blk.empty()) return PS_OK;
@@ -363,6 +364,126 @@ int32_t ps_kv_stage_out(const ps_layout* lay, const void* dev_tables, const void
 int32_t ps_kv_stage_in(const ps_layout* lay, const void* dev_tables, const void* image, void* kv_pool, float* kv_scales,
                        void* stream) {
   return stage(lay, dev_tables, false, kv_pool, kv_scales, const_cast<void*>(image), stream);
+}
+
+namespace {
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int32_t check_rope(const ps_geometry& g, const ps_rope* rope) {
+  if (!rope || !(rope->eps >= 0.f) || std::isinf(rope->eps) || rope->rot_dim < 0 || rope->rot_dim > g.head_dim || rope->rot_dim % 2 != 0)
+    return PS_ERR_INVALID_ARG;
+  if (rope->pairing != PS_ROPE_HALVES && rope->pairing != PS_ROPE_NEIGHBOURS) return PS_ERR_INVALID_ARG;
+  if (rope->rot_dim > 0 && !rope->turns) return PS_ERR_INVALID_ARG;
+  if (!psdev::rope_supported(g) || (rope->pairing == PS_ROPE_HALVES && rope->rot_dim % 16 != 0)) return PS_ERR_UNSUPPORTED;
+  if (!aligned16(rope->q_weight) || !aligned16(rope->k_weight) || reinterpret_cast<uintptr_t>(rope->turns) % 8) return PS_ERR_SHAPE;
+  return PS_OK;
+}
+
+psdev::RopeArgs rope_args(const ps_rope& r, const int32_t* positions) {
+  return {r.turns, r.q_weight, r.k_weight, positions, r.eps, r.rot_dim, r.pairing == PS_ROPE_NEIGHBOURS};
+}
+
+// Strides of rows of `dtype` elements, a head's `head_dim` of them in a row.
+bool rows_addressable(const ps_geometry& g, int dtype, const void* p, int64_t s_row, int64_t s_head) {
+  const int64_t esz = dtype == PS_F32 ? 4 : 2;
+  return aligned16(p) && s_row >= g.head_dim && s_head >= g.head_dim && (s_row * esz) % 16 == 0 && (s_head * esz) % 16 == 0;
+}
+
+}  // namespace
+
+int32_t ps_rope_rows(const ps_geometry* g, const ps_rope* rope, int64_t num_rows, const void* src, int64_t src_stride_row,
+                     int64_t src_stride_head, const int32_t* positions, void* out, void* stream) {
+  if (!g || num_rows < 0) return PS_ERR_INVALID_ARG;
+  if (g->num_q_heads <= 0) return PS_ERR_SHAPE;
+  if (g->q_dtype != PS_F32 && g->q_dtype != PS_BF16) return PS_ERR_UNSUPPORTED;
+  if (int32_t rc = check_rope(*g, rope)) return rc;
+  if (num_rows == 0) return PS_OK;
+  if (!src || !positions || !out) return PS_ERR_INVALID_ARG;
+  if (!rows_addressable(*g, g->q_dtype, src, src_stride_row, src_stride_head) || !aligned16(out)) return PS_ERR_SHAPE;
+  if (int32_t rc = psdev::launch_rope_rows(rope_args(*rope, positions), *g, src, src_stride_row, src_stride_head, num_rows, out,
+                                           static_cast<hipStream_t>(stream)))
+    return rc;
+  return check_hip(hipGetLastError());
+}
+
+int32_t ps_kv_append_rope(const ps_layout* lay, const void* dev_tables, const ps_rope* rope, const ps_token_rows* rows, void* q_out,
+                          void* kv_pool, float* kv_scales, void* stream) {
+  if (!lay || !dev_tables || !rows || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
+  const ps_geometry& g = lay->geo;
+  if (int32_t rc = check_rope(g, rope)) return rc;
+  if (lay->num_requests == 0) return PS_OK;
+  if (!rows->k || !rows->v || !rows->positions || !kv_pool || (rows->q == nullptr) != (q_out == nullptr) ||
+      (g.kv_dtype == PS_FP8_E4M3 && !kv_scales))
+    return PS_ERR_INVALID_ARG;
+  const int kv_src = g.kv_dtype == PS_F32 ? PS_F32 : PS_BF16;
+  if (!rows_addressable(g, kv_src, rows->k, rows->kv_stride_row, rows->kv_stride_head) || !aligned16(rows->v) || !aligned16(kv_pool) ||
+      (rows->q && (!rows_addressable(g, g.q_dtype, rows->q, rows->q_stride_row, rows->q_stride_head) || !aligned16(q_out))))
+    return PS_ERR_SHAPE;
+  if (int32_t rc = psdev::launch_append_rope(lay, dev_tables, rope_args(*rope, rows->positions), *rows, q_out, kv_pool, kv_scales,
+                                             static_cast<hipStream_t>(stream)))
+    return rc;
+  return check_hip(hipGetLastError());
+}
+
+int32_t ps_kv_ingest_rope(const ps_layout* lay, const void* dev_tables, int32_t which, const ps_rope* rope, const void* src_k,
+                          const void* src_v, int64_t src_stride_tok, int64_t src_stride_head, const int32_t* positions,
+                          void* kv_pool, float* kv_scales, void* stream) {
+  if (!lay || !dev_tables || which < 0 || which > 2 || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
+  const ps_geometry& g = lay->geo;
+  if (int32_t rc = check_rope(g, rope)) return rc;
+  const size_t entries = which == 0 ? lay->prefix_blk.size() : (which == 1 ? lay->suffix_blk.size() : lay->root_blk.size());
+  if (entries == 0) return PS_OK;
+  if (!src_k || !src_v || !positions || !kv_pool || (g.kv_dtype == PS_FP8_E4M3 && !kv_scales)) return PS_ERR_INVALID_ARG;
+  const int src = g.kv_dtype == PS_F32 ? PS_F32 : PS_BF16;
+  if (!rows_addressable(g, src, src_k, src_stride_tok, src_stride_head) || !aligned16(src_v) || !aligned16(kv_pool)) return PS_ERR_SHAPE;
+  if (int32_t rc = psdev::launch_ingest_rope(lay, dev_tables, which, rope_args(*rope, positions), src_k, src_v, src_stride_tok,
+                                             src_stride_head, kv_pool, kv_scales, static_cast<hipStream_t>(stream)))
+    return rc;
+  return check_hip(hipGetLastError());
+}
+
+int32_t ps_kv_gather(const ps_layout* lay, const void* dev_tables, int32_t which, const void* kv_pool, const float* kv_scales,
+                     int32_t dst_dtype, void* dst_k, void* dst_v, int64_t dst_stride_tok, int64_t dst_stride_head, void* stream) {
+  if (!lay || !dev_tables || which < 0 || which > 2 || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
+  if (dst_dtype != PS_F32 && dst_dtype != PS_BF16) return PS_ERR_UNSUPPORTED;
+  const ps_geometry& g = lay->geo;
+  const size_t entries = which == 0 ? lay->prefix_blk.size() : (which == 1 ? lay->suffix_blk.size() : lay->root_blk.size());
+  if (entries == 0) return PS_OK;
+  if (!dst_k || !dst_v || !kv_pool || (g.kv_dtype == PS_FP8_E4M3 && !kv_scales)) return PS_ERR_INVALID_ARG;
+  if (!rows_addressable(g, dst_dtype, dst_k, dst_stride_tok, dst_stride_head) || !aligned16(dst_v) || !aligned16(kv_pool)) return PS_ERR_SHAPE;
+  if (int32_t rc = psdev::launch_kv_gather(lay, dev_tables, which, kv_pool, kv_scales, dst_dtype, dst_k, dst_v, dst_stride_tok,
+                                           dst_stride_head, static_cast<hipStream_t>(stream)))
+    return rc;
+  return check_hip(hipGetLastError());
+}
+
+int32_t ps_block_summaries(const ps_layout* lay, const void* dev_tables, int32_t which, const void* kv_pool, const float* kv_scales,
+                           int8_t* summaries, float* summary_scales, void* stream) {
+  if (!lay || !dev_tables || which < 0 || which > 2 || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
+  const ps_geometry& g = lay->geo;
+  if (!psdev::rope_supported(g)) return PS_ERR_UNSUPPORTED;
+  const size_t entries = which == 0 ? lay->prefix_blk.size() : (which == 1 ? lay->suffix_blk.size() : lay->root_blk.size());
+  if (entries == 0) return PS_OK;
+  if (!kv_pool || !summaries || !summary_scales || (g.kv_dtype == PS_FP8_E4M3 && !kv_scales)) return PS_ERR_INVALID_ARG;
+  if (!aligned16(kv_pool) || !aligned16(summaries)) return PS_ERR_SHAPE;
+  if (int32_t rc = psdev::launch_block_summaries(lay, dev_tables, which, kv_pool, kv_scales, summaries, summary_scales,
+                                                 static_cast<hipStream_t>(stream)))
+    return rc;
+  return check_hip(hipGetLastError());
+}
+
+int32_t ps_select_blocks(const ps_layout* base, const void* base_tables, const ps_layout* sel, void* selection_tables, const void* q,
+                         const int8_t* summaries, const float* summary_scales, void* workspace, void* stream) {
+  if (!base || !base_tables || !sel || !selection_tables || !sel->sel || base->parked || sel->parked) return PS_ERR_INVALID_ARG;
+  if (sel->sel->base_id != base->id || sel->sel->base_version != base->version) return PS_ERR_INVALID_ARG;
+  if (sel->sel->choices.empty()) return PS_OK;
+  if (!q || !summaries || !summary_scales || !workspace) return PS_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(summaries) || !aligned16(workspace)) return PS_ERR_SHAPE;
+  if (int32_t rc = psdev::launch_select_blocks(base, base_tables, sel, selection_tables, q, summaries, summary_scales,
+                                               static_cast<float*>(workspace), static_cast<hipStream_t>(stream)))
+    return rc;
+  return check_hip(hipGetLastError());
 }
 
 int32_t ps_probe_read(const void* dev_buf, int64_t bytes, int32_t pattern, int32_t num_workgroups, void* stream) {

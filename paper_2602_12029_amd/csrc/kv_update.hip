@@ -14,52 +14,12 @@
 #include <type_traits>
 
 #include "device_common.h"
+#include "kv_common.h"
 #include "launch.h"
 
 namespace psdev {
 
 namespace {
-
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-
-// Bulk K/V passes through these kernels once and is far larger than the caches: loads and stores are non-temporal,
-// so the lines neither displace what the caches hold nor wait there for a reader that never comes.
-template <typename V>
-__device__ __forceinline__ V stream_load(const V* p) { return __builtin_nontemporal_load(p); }
-template <typename V>
-__device__ __forceinline__ void stream_store(V* p, V v) { __builtin_nontemporal_store(v, p); }
-
-// e4m3fn code -> float32 (exact)
-__device__ __forceinline__ float e4m3_to_f32(uint32_t code) {
-  const uint32_t e = (code >> 3) & 0xf, m = code & 7;
-  const float mag = e ? __uint_as_float(((e + 120u) << 23) | (m << 20)) : float(m) * 0x1p-9f;
-  return (code & 0x80) ? -mag : mag;
-}
-
-// two float32 -> two e4m3fn codes in the low 16 bits (v_cvt_pk_fp8_f32: nearest even).  Inputs never reach the
-// midpoint above 448 here (|x| <= tile maximum), so saturation behaviour is not relied upon.
-__device__ __forceinline__ uint32_t f32x2_to_e4m3(float a, float b) {
-  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false)) & 0xffffu;
-}
-
-__device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, lane_xor(x, m));
-  return x;
-}
-
-struct KvWriteParams {
-  const int32_t* blk;        // concatenated block array
-  const int32_t* ent_tok0;   // per entry: its first token in the ragged source of its kind
-  const int32_t* ent_valid;  // per entry: tokens stored in the block
-  const int32_t* ent_order;  // per entry position: the entry an ingest or stage-in takes there (shared kinds by physical block)
-  const int32_t* dest;       // [R] block * B + slot of the token being appended, -1 = none
-  void* kv;
-  float* scales;
-  int32_t num_kv_heads, head_dim, block_size;
-  int64_t s_block, s_head, s_kv, s_tok;  // pool strides, elements
-};
 
 // ---- ingest, storage formats that keep the source bits (T = uint16_t for bf16, float) --------------------
 // One wavefront per piece of an (entry, head, K|V) tile: 256 16-byte chunks, four a lane, all fetched before the first
@@ -156,54 +116,18 @@ __global__ __launch_bounds__(256) void ingest_e4m3_kernel(KvWriteParams p, const
   amax = wave_max(amax);
   const float scale = amax > 0.f ? amax / 448.f : 1.f;
   if (lane == 0) p.scales[(int64_t(id) * p.num_kv_heads + h) * 2 + which] = scale;
-  // x / scale without a division per element.  q0 = x * RN(1 / scale) is within 2 ulp of the exact quotient and
-  // the correctly rounded quotient within 0.5 ulp, so both lie on the same side of every rounding boundary of
-  // e4m3 -- and get the same code -- unless q0 is within a few ulp of one.  Boundaries (midpoints of neighbouring
-  // e4m3 values) have the float32 pattern "3 mantissa bits, then 1000...0" in the normal range; a chunk in which
-  // any lane is that close to one, or may fall into the subnormal range of e4m3 (an absolute grid), is redone with
-  // the real division.  The stored codes are therefore exactly those of RN(x / scale) everywhere.
-  const float rinv = 1.f / scale;
-  const float subnormal_below = scale * 0x1.000002p-6f;   // |x| under this: the quotient may be under 2^-6
+  const E4m3Encoder encode(scale);
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = lane + 64 * i;
-    float x[8], q[8];
-    bool risky = false;
+    float x[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       x[2 * j] = bf16_bits_to_f32(raw[i][j] & 0xffffu);
       x[2 * j + 1] = bf16_bits_to_f32(raw[i][j] >> 16);
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      q[j] = x[j] * rinv;
-      // low 20 mantissa bits within [0x7fffc, 0x80004]: shifted to the top of the word, offset so the window starts at 0
-      risky |= (__float_as_uint(q[j]) << 12) + 0x80004000u <= 0x8000u;
-      risky |= fabsf(x[j]) < subnormal_below;               // subnormal range of e4m3 (also catches exact zeros)
-    }
-    risky = risky && c < total;                               // lanes past the tile hold zeros: no say
-    if (__builtin_amdgcn_ballot_w64(risky) != 0) {
-      // second look: a quotient near a boundary that is exact (zero residual x - q0 * scale; ties of short
-      // mantissas are common with bf16 inputs) is the correctly rounded quotient already
-      bool divide = false;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool near = (__float_as_uint(q[j]) << 12) + 0x80004000u <= 0x8000u;
-        divide |= near && __builtin_fmaf(-q[j], scale, x[j]) != 0.f;
-        divide |= fabsf(x[j]) < subnormal_below;
-      }
-      divide = divide && c < total;
-      if (__builtin_amdgcn_ballot_w64(divide) != 0) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = x[j] / scale;
-      }
-    }
-    if (c < total) {
-      u32x2 out;
-      out[0] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), true));
-      out[1] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[6], q[7], __builtin_amdgcn_cvt_pk_fp8_f32(q[4], q[5], 0, false), true));
-      stream_store(reinterpret_cast<u32x2*>(dst + int64_t(token_of(c)) * p.s_tok + column_of(c)), out);
-    }
+    const u32x2 out = encode(x, c < total);                   // lanes past the tile hold zeros: no say
+    if (c < total) stream_store(reinterpret_cast<u32x2*>(dst + int64_t(token_of(c)) * p.s_tok + column_of(c)), out);
   }
 }
 
@@ -229,63 +153,22 @@ __global__ __launch_bounds__(256) void append_copy_kernel(KvWriteParams p, const
   if (dest >= 0) append_copy_row(p, new_k, new_v, dest, r, int((row >> 1) % p.num_kv_heads), int(row & 1));
 }
 
-// e4m3 with rows of 2^row_shift eight-element pieces: one wavefront per (request, kv head, K|V), eight elements a lane.  The
-// stored tokens of a tile whose scale has grown are rewritten 64 >> row_shift at a time, and four of those rounds are fetched
-// together: a block of sixteen 128-wide tokens in one round trip (a byte at a time the launch was bound by the chain of those
-// rewrites: 64 requests, eight heads, tokens of changing magnitude 8.5 -> 5.2 us).
+// e4m3 with rows of 2^row_shift eight-element pieces: one wavefront per (request, kv head, K|V), eight elements a lane.
 __device__ __forceinline__ void append_e4m3x8_row(const KvWriteParams& p, const u32x4* __restrict__ new_k, const u32x4* __restrict__ new_v,
                                                   int row_shift, int dest, int r, int h, int which) {
   const int lane = threadIdx.x & 63;
-  const int id = dest / p.block_size, slot = dest % p.block_size;
-  uint8_t* tile = static_cast<uint8_t*>(p.kv) + int64_t(id) * p.s_block + int64_t(h) * p.s_head + int64_t(which) * p.s_kv;
-  float* scale_ptr = p.scales + (int64_t(id) * p.num_kv_heads + h) * 2 + which;
-  const int c = lane & ((1 << row_shift) - 1), tok0 = lane >> row_shift, toks = 64 >> row_shift;
+  const E4m3Tile tile = e4m3_tile(p, dest, h, which);
+  const int c = lane & ((1 << row_shift) - 1);
   // (every token group of the wave holds the whole row)
   const u32x4 raw = (which ? new_v : new_k)[((int64_t(r) * p.num_kv_heads + h) << row_shift) + c];
-  const float old = *scale_ptr;   // (of a fresh block: anything, and not used)
-  float x[8], amax = 0.f;
+  const float old = *tile.scale;   // (of a fresh block: anything, and not used)
+  float x[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     x[2 * j] = bf16_bits_to_f32(raw[j] & 0xffffu);
     x[2 * j + 1] = bf16_bits_to_f32(raw[j] >> 16);
-    amax = fmaxf(amax, fmaxf(fabsf(x[2 * j]), fabsf(x[2 * j + 1])));
   }
-  amax = wave_max(amax);
-  const float cand = amax / 448.f;
-  float scale;
-  auto encode = [](const float (&y)[8]) {
-    u32x2 out;
-    out[0] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true));
-    out[1] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false), true));
-    return out;
-  };
-  if (slot == 0) {
-    scale = amax > 0.f ? cand : 1.f;
-  } else {
-    scale = fmaxf(old, cand);
-    if (scale != old) {   // the tile's scale grew: re-encode what is stored, from the stored values
-      for (int t0 = tok0; t0 < slot; t0 += 4 * toks) {
-        u32x2 code[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (t0 + u * toks < slot) code[u] = *reinterpret_cast<const u32x2*>(tile + int64_t(t0 + u * toks) * p.s_tok + 8 * c);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (t0 + u * toks < slot) {
-            float y[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = (e4m3_to_f32((code[u][j >> 2] >> (8 * (j & 3))) & 0xffu) * old) / scale;
-            *reinterpret_cast<u32x2*>(tile + int64_t(t0 + u * toks) * p.s_tok + 8 * c) = encode(y);
-          }
-      }
-    }
-  }
-  if (lane == 0) *scale_ptr = scale;
-  if (tok0 == 0) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = x[j] / scale;
-    *reinterpret_cast<u32x2*>(tile + int64_t(slot) * p.s_tok + 8 * c) = encode(x);
-  }
+  append_e4m3x8_values(p, tile, x, old, row_shift);
 }
 
 __global__ __launch_bounds__(256) void append_e4m3x8_kernel(KvWriteParams p, const u32x4* __restrict__ new_k,
@@ -438,27 +321,6 @@ __global__ __launch_bounds__(256) void stage_copy_kernel(KvWriteParams p, uint8_
         }
       }
   }
-}
-
-KvWriteParams make_write_params(const ps_layout* lay, const void* dev_tables, void* kv, float* scales) {
-  const int32_t* t = static_cast<const int32_t*>(dev_tables);
-  const ps_geometry& g = lay->geo;
-  KvWriteParams p{};
-  p.blk = t + lay->off_blk;
-  p.ent_tok0 = t + lay->off_ent_tok0;
-  p.ent_valid = t + lay->off_ent_valid;
-  p.ent_order = t + lay->off_ent_order;
-  p.dest = t + lay->off_dest;
-  p.kv = kv;
-  p.scales = scales;
-  p.num_kv_heads = g.num_kv_heads;
-  p.head_dim = g.head_dim;
-  p.block_size = g.block_size;
-  p.s_block = g.kv_stride_block;
-  p.s_head = g.kv_stride_head;
-  p.s_kv = g.kv_stride_kv;
-  p.s_tok = g.kv_stride_tok;
-  return p;
 }
 
 }  // namespace

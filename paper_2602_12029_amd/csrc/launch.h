@@ -44,4 +44,29 @@ int32_t launch_probe_read(const void* buf, int64_t bytes, int pattern, int num_w
 int32_t launch_merge(const int32_t* slot_base, const int32_t* requests, const float* ws_o, const float* ws_lse, void* out,
                      float* out_lse, int num_requests, int max_states, const ps_geometry& g, hipStream_t st);
 
+// Norm and rotation of head rows (rope.hip): the parameters of ps_rope and the rows' positions.
+struct RopeArgs {
+  const uint64_t* turns;
+  const void *q_weight, *k_weight;
+  const int32_t* positions;
+  float eps;
+  int32_t rot;
+  bool neighbours;
+};
+inline bool rope_supported(const ps_geometry& g) { return g.head_dim == 64 || g.head_dim == 128 || g.head_dim == 256; }
+int32_t launch_rope_rows(const RopeArgs& a, const ps_geometry& g, const void* src, int64_t s_row, int64_t s_head, int64_t num_rows,
+                         void* out, hipStream_t st);
+int32_t launch_append_rope(const ps_layout* lay, const void* dev_tables, const RopeArgs& a, const ps_token_rows& rows, void* q_out,
+                           void* kv, float* scales, hipStream_t st);
+int32_t launch_ingest_rope(const ps_layout* lay, const void* dev_tables, int which, const RopeArgs& a, const void* src_k,
+                           const void* src_v, int64_t s_tok, int64_t s_head, void* kv, float* scales, hipStream_t st);
+// Stored segments back into contiguous tensors, and the per-block summaries of the keys (kv_read.hip).
+int32_t launch_kv_gather(const ps_layout* lay, const void* dev_tables, int which, const void* kv, const float* scales, int dst_dtype,
+                         void* dst_k, void* dst_v, int64_t s_tok, int64_t s_head, hipStream_t st);
+int32_t launch_block_summaries(const ps_layout* lay, const void* dev_tables, int which, const void* kv, const float* scales,
+                               int8_t* summaries, float* summary_scales, hipStream_t st);
+// Scores of the blocks that a selection's requests choose from, and the choice (select.hip).
+int32_t launch_select_blocks(const ps_layout* base, const void* dev_tables, const ps_layout* sel, void* sel_tables, const void* q,
+                             const int8_t* summaries, const float* summary_scales, float* scores, hipStream_t st);
+
 }  // namespace psdev

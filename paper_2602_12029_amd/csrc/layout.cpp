@@ -6,6 +6,7 @@
 // only the model-specific segment is private (Efficiency Analysis Eq. 9).
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <map>
@@ -113,6 +114,12 @@ static void find_solo_items(ps_layout* lay) {
   lay->num_solo_items = 0;
   if (lay->solo_limit > 0)
     for (size_t i = lay->items.size(); i-- > size_t(lay->num_prefix_items) && !too_long(lay->items[i]);) ++lay->num_solo_items;
+}
+
+// A selection's block array is there once per KV head: moves every item's blk_off by `stride` words a head.
+static void shift_heads(ps_layout* lay, int64_t stride) {
+  for (std::vector<ps_item>* items : {&lay->items, &lay->pk_prefix.items, &lay->pk_suffix.items, &lay->pk_all.items})
+    for (ps_item& it : *items) it.blk_off += int32_t(it.kv_head * stride);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -876,6 +883,7 @@ static int32_t build_plan(ps_layout* lay, const ps_plan_options* user, bool fewe
   lay->pk_prefix = pre_mfma ? pack(first_packed, lay->num_prefix_items, false) : packed{};
   lay->pk_suffix = suf_mfma ? pack(lay->num_prefix_items, n_items, false) : packed{};
   lay->pk_all = (pre_mfma && suf_mfma) ? pack(first_packed, n_items, true) : packed{};
+  if (lay->sel) shift_heads(lay, lay->head_stride);
   return ps_blob_build(lay);
 }
 
@@ -908,8 +916,10 @@ int32_t ps_blob_build(ps_layout* lay) {
   // [slot_base][visible][requests to merge][schedules]
   // [per-block source offsets and valid counts][destinations of the last append]
   auto pad4 = [](int64_t n) { return (n + 3) / 4 * 4; };
+  ++lay->version;
   lay->off_blk = 0;
-  lay->off_req = pad4(lay->off_blk + int64_t(lay->prefix_blk.size() + lay->suffix_blk.size() + lay->root_blk.size()));
+  const int64_t all_blk = int64_t(lay->prefix_blk.size() + lay->suffix_blk.size() + lay->root_blk.size());
+  lay->off_req = pad4(lay->off_blk + (lay->sel ? lay->head_stride * g.num_kv_heads : all_blk));
   lay->off_items = pad4(lay->off_req + int64_t(lay->req_list.size()));
   lay->off_slot = pad4(lay->off_items + 8 * int64_t(lay->items.size()));
   lay->off_visible = pad4(lay->off_slot + R + 1);
@@ -933,12 +943,17 @@ int32_t ps_blob_build(ps_layout* lay) {
   place(lay->sched_prefix, pk_prefix);
   place(lay->sched_suffix, pk_suffix);
   place(lay->sched_all, pk_all);
-  // per-block directory for the cache-writing kernels
-  const int64_t num_blk_entries = int64_t(lay->prefix_blk.size() + lay->suffix_blk.size() + lay->root_blk.size());
+  if (lay->sel) {
+    lay->sel->off_choices = words;
+    lay->sel->off_score_items = pad4(words + int64_t(lay->sel->choices.size()));
+    words = pad4(lay->sel->off_score_items + int64_t(lay->sel->score_items.size()));
+  }
+  // per-block directory for the cache-writing kernels (which a selection has no use for)
+  const int64_t num_blk_entries = lay->sel ? 0 : all_blk;
   lay->off_ent_tok0 = words;
   lay->off_ent_valid = pad4(lay->off_ent_tok0 + num_blk_entries);
   lay->off_dest = pad4(lay->off_ent_valid + num_blk_entries);
-  lay->off_ent_order = pad4(lay->off_dest + R);
+  lay->off_ent_order = pad4(lay->off_dest + (lay->sel ? 0 : R));
   words = pad4(lay->off_ent_order + num_blk_entries);
   // (the tables grow by a few words per decode step: room to spare keeps the buffer -- and its mapped pages -- in
   // place instead of taking a fresh allocation every step)
@@ -946,7 +961,7 @@ int32_t ps_blob_build(ps_layout* lay) {
   if (lay->blob.capacity() < blob_words) lay->blob.reserve(blob_words + blob_words / 4 + 1024);
   lay->blob.resize(blob_words);   // (every word that a kernel reads is written below)
   int32_t* b = lay->blob.data();
-  {
+  if (!lay->sel) {
     const int32_t B = g.block_size;
     // skip: per segment, leading blocks that are not to be written (adopted from another layout); the ragged source
     // then holds only the tokens after them
@@ -1032,6 +1047,11 @@ int32_t ps_blob_build(ps_layout* lay) {
   std::copy(lay->prefix_blk.begin(), lay->prefix_blk.end(), b + lay->off_blk);
   std::copy(lay->suffix_blk.begin(), lay->suffix_blk.end(), b + lay->off_blk + lay->prefix_blk.size());
   std::copy(lay->root_blk.begin(), lay->root_blk.end(), b + lay->off_blk + root_blk0);
+  if (lay->sel) {
+    for (int32_t h = 1; h < g.num_kv_heads; ++h) std::copy(b + lay->off_blk, b + lay->off_blk + all_blk, b + lay->off_blk + h * lay->head_stride);
+    std::copy(lay->sel->choices.begin(), lay->sel->choices.end(), b + lay->sel->off_choices);
+    std::copy(lay->sel->score_items.begin(), lay->sel->score_items.end(), b + lay->sel->off_score_items);
+  }
   std::copy(lay->req_list.begin(), lay->req_list.end(), b + lay->off_req);
   for (int32_t r = 0; r < R; ++r) b[lay->off_visible + r] = visible_of(r);
   std::copy(lay->merge_req.begin(), lay->merge_req.end(), b + lay->off_merge);
@@ -1340,7 +1360,7 @@ int32_t ps_layout_root_tables(const ps_layout* lay, int32_t* num_roots, const in
 
 int32_t ps_layout_release(ps_pool* pool, ps_layout* lay) {
   if (!pool || !lay) return PS_ERR_INVALID_ARG;
-  if (!lay->parked)
+  if (!lay->parked && !lay->sel)
     if (int32_t st = drop_references(pool, lay)) return st;
   delete lay;
   return PS_OK;
@@ -1364,7 +1384,7 @@ int32_t ps_blocks_needed(int32_t block_size, int32_t num_roots, const int32_t* r
 }
 
 int32_t ps_layout_park(ps_pool* pool, ps_layout* lay) {
-  if (!pool || !lay || lay->parked) return PS_ERR_INVALID_ARG;
+  if (!pool || !lay || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
   if (int32_t st = drop_references(pool, lay)) return st;
   lay->parked = true;
   lay->adopt_indptr.clear();   // a resumed layout holds fresh blocks only: its image carries the adopted contents
@@ -1380,7 +1400,7 @@ int32_t ps_layout_park(ps_pool* pool, ps_layout* lay) {
 }
 
 int32_t ps_layout_resume(ps_pool* pool, ps_layout* lay) {
-  if (!pool || !lay || !lay->parked) return PS_ERR_INVALID_ARG;
+  if (!pool || !lay || !lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
   if (blocks_of(lay) > int64_t(pool->free_list.size())) return PS_ERR_OOM;
   take_blocks(pool, lay);
   lay->parked = false;
@@ -1392,13 +1412,13 @@ int32_t ps_layout_resume(ps_pool* pool, ps_layout* lay) {
 
 int32_t ps_layout_state(const ps_layout* lay, int64_t* num_blocks, int32_t* parked) {
   if (!lay) return PS_ERR_INVALID_ARG;
-  if (num_blocks) *num_blocks = blocks_of(lay);
+  if (num_blocks) *num_blocks = lay->sel ? 0 : blocks_of(lay);   // (a selection holds none)
   if (parked) *parked = lay->parked ? 1 : 0;
   return PS_OK;
 }
 
 int32_t ps_stage_layout(const ps_layout* lay, int64_t* block_bytes, int64_t* scales_offset_bytes, int64_t* total_bytes) {
-  if (!lay) return PS_ERR_INVALID_ARG;
+  if (!lay || lay->sel) return PS_ERR_INVALID_ARG;
   const ps_geometry& g = lay->geo;
   const int64_t esz = g.kv_dtype == PS_F32 ? 4 : (g.kv_dtype == PS_BF16 ? 2 : 1);
   const int64_t per_block = int64_t(g.num_kv_heads) * 2 * g.block_size * g.head_dim * esz;
@@ -1430,8 +1450,60 @@ int32_t ps_layout_lengths(const ps_layout* lay, const int32_t** prefix_len, cons
   return PS_OK;
 }
 
+}  // extern "C"
+
+// The plan after private segments have grown by a token each where grew(r); old_stride: a selection's head_stride before that.
+template <typename Grew>
+static int32_t plan_growth(ps_layout* lay, const Grew& grew, int64_t old_stride) {
+  // A step that leaves the chunk structure of every private segment as it is (same number of chunks, same chunk
+  // size where there are several) only moves token ends and block offsets: the plan -- items, their order, the
+  // packing onto workgroups -- is kept and patched, and only the tables are laid out again.  Anything else (a first
+  // token, a segment outgrowing its chunks, a schedule its balance) plans afresh.
+  const int32_t R = lay->num_requests, B = lay->geo.block_size;
+  bool same_structure = lay->suffix_chunks.size() == size_t(R) && lay->suffix_chunk > 0;
+  const int64_t granule = std::lcm<int64_t>(B, 32);
+  for (int32_t r = 0; r < R && same_structure; ++r) {
+    if (!grew(r)) continue;
+    const int64_t len = lay->suffix_len[size_t(r)];
+    const int64_t count = ceil_div(len, lay->suffix_chunk);
+    const int64_t size = round_up(ceil_div(len, count), granule);
+    const int64_t n = ceil_div(len, size);
+    if (len <= 1 || n != lay->suffix_chunks[size_t(r)] || (n > 1 && size != lay->suffix_chunk_size[size_t(r)]))
+      same_structure = false;
+    else
+      lay->suffix_chunk_size[size_t(r)] = int32_t(size);
+  }
+  if (same_structure) {
+    const int32_t prefix_blocks = int32_t(lay->prefix_blk.size());
+    const int32_t root_shift = int32_t(lay->prefix_blk.size() + lay->suffix_blk.size()) - lay->planned_root_blk0;
+    auto patch = [&](std::vector<ps_item>& items) {
+      for (ps_item& it : items) {
+        it.blk_off -= int32_t(it.kv_head * old_stride);
+        if (it.kind & kPsItemSuffix) {
+          const int32_t r = it.req_off - R;   // private-suffix items index the identity part of the request list
+          it.blk_off = prefix_blocks + lay->suffix_blk_indptr[size_t(r)];
+          it.tok_end = std::min(lay->suffix_len[size_t(r)], it.tok_begin + lay->suffix_chunk_size[size_t(r)]);
+        } else if (it.kind & kPsItemRoot) {
+          it.blk_off += root_shift;
+        }
+      }
+    };
+    patch(lay->items);
+    patch(lay->pk_prefix.items);
+    patch(lay->pk_suffix.items);
+    patch(lay->pk_all.items);
+    if (lay->sel) shift_heads(lay, lay->head_stride);
+    lay->planned_root_blk0 += root_shift;
+    find_solo_items(lay);
+    same_structure = !outgrown(lay);
+  }
+  return same_structure ? ps_blob_build(lay) : ps_plan_build(lay, &lay->opt);
+}
+
+extern "C" {
+
 int32_t ps_layout_append(ps_pool* pool, ps_layout* lay, const int32_t* active, const int32_t** dest) {
-  if (!pool || !lay || lay->parked) return PS_ERR_INVALID_ARG;
+  if (!pool || !lay || lay->parked || lay->sel) return PS_ERR_INVALID_ARG;
   const int32_t R = lay->num_requests, B = lay->geo.block_size;
   if (int64_t(pool->num_blocks) * B > INT32_MAX) return PS_ERR_INVALID_ARG;  // slot indices are int32
   auto is_active = [&](int32_t r) { return !active || active[r] != 0; };
@@ -1466,52 +1538,13 @@ int32_t ps_layout_append(ps_pool* pool, ps_layout* lay, const int32_t* active, c
   }
   lay->suffix_blk.swap(blk);
   lay->suffix_blk_indptr.swap(indptr);
-  // A step that leaves the chunk structure of every private segment as it is (same number of chunks, same chunk
-  // size where there are several) only moves token ends and block offsets: the plan -- items, their order, the
-  // packing onto workgroups -- is kept and patched, and only the tables are laid out again.  Anything else (a first
-  // token, a segment outgrowing its chunks, a schedule its balance) plans afresh.
-  bool same_structure = lay->suffix_chunks.size() == size_t(R) && lay->suffix_chunk > 0;
-  const int64_t granule = std::lcm<int64_t>(B, 32);
-  for (int32_t r = 0; r < R && same_structure; ++r) {
-    if (!is_active(r)) continue;
-    const int64_t len = lay->suffix_len[size_t(r)];
-    const int64_t count = ceil_div(len, lay->suffix_chunk);
-    const int64_t size = round_up(ceil_div(len, count), granule);
-    const int64_t n = ceil_div(len, size);
-    if (len <= 1 || n != lay->suffix_chunks[size_t(r)] || (n > 1 && size != lay->suffix_chunk_size[size_t(r)]))
-      same_structure = false;
-    else
-      lay->suffix_chunk_size[size_t(r)] = int32_t(size);
-  }
-  if (same_structure) {
-    const int32_t prefix_blocks = int32_t(lay->prefix_blk.size());
-    const int32_t root_shift = int32_t(lay->prefix_blk.size() + lay->suffix_blk.size()) - lay->planned_root_blk0;
-    auto patch = [&](std::vector<ps_item>& items) {
-      for (ps_item& it : items) {
-        if (it.kind & kPsItemSuffix) {
-          const int32_t r = it.req_off - R;   // private-suffix items index the identity part of the request list
-          it.blk_off = prefix_blocks + lay->suffix_blk_indptr[size_t(r)];
-          it.tok_end = std::min(lay->suffix_len[size_t(r)], it.tok_begin + lay->suffix_chunk_size[size_t(r)]);
-        } else if (it.kind & kPsItemRoot) {
-          it.blk_off += root_shift;
-        }
-      }
-    };
-    patch(lay->items);
-    patch(lay->pk_prefix.items);
-    patch(lay->pk_suffix.items);
-    patch(lay->pk_all.items);
-    lay->planned_root_blk0 += root_shift;
-    find_solo_items(lay);
-    same_structure = !outgrown(lay);
-  }
-  if (int32_t st = same_structure ? ps_blob_build(lay) : ps_plan_build(lay, &lay->opt)) return st;
+  if (int32_t st = plan_growth(lay, is_active, 0)) return st;
   if (dest) *dest = lay->append_dest.data();
   return PS_OK;
 }
 
 int32_t ps_layout_set_visible(ps_layout* lay, const int32_t* prefix_visible) {
-  if (!lay) return PS_ERR_INVALID_ARG;
+  if (!lay || lay->sel) return PS_ERR_INVALID_ARG;
   std::vector<int32_t> v;
   if (prefix_visible) {
     v.assign(prefix_visible, prefix_visible + lay->num_requests);
@@ -1587,6 +1620,222 @@ const char* ps_strerror(int32_t status) {
     case PS_ERR_TOO_LARGE: return "the batch's partial states exceed the library's static workspace (PS_STATIC_WORKSPACE_BYTES)";
     default: return "unknown status";
   }
+}
+
+}  // extern "C"
+
+namespace {
+
+// What a selection holds of its base's batch: every request a prompt of its own, its prefix the blocks it attends to, a partly
+// filled last root block a root of its own (it would end inside the list otherwise), its private segment as it is.
+int32_t derive_selection(const ps_layout* base, ps_layout* lay) {
+  const int32_t R = base->num_requests, B = base->geo.block_size, H = base->geo.num_kv_heads;
+  const ps_select_options& opt = lay->sel->opt;
+  const int32_t root_blk0 = int32_t(base->prefix_blk.size() + base->suffix_blk.size());
+  lay->geo = base->geo;
+  lay->num_prompts = lay->num_requests = R;
+  lay->prefix_len.assign(size_t(R), 0);
+  lay->suffix_len = base->suffix_len;
+  lay->req_model = base->req_model;
+  lay->req_prompt.resize(size_t(R));
+  std::iota(lay->req_prompt.begin(), lay->req_prompt.end(), 0);
+  lay->group_req = lay->req_prompt;
+  lay->group_indptr.resize(size_t(R) + 1);
+  std::iota(lay->group_indptr.begin(), lay->group_indptr.end(), 0);
+  lay->prefix_blk.clear();
+  lay->prefix_blk_indptr.assign(size_t(R) + 1, 0);
+  lay->suffix_blk = base->suffix_blk;
+  lay->suffix_blk_indptr = base->suffix_blk_indptr;
+  lay->num_roots = 0;
+  lay->root_len.clear();
+  lay->root_blk.clear();
+  lay->root_blk_indptr.assign(1, 0);
+  lay->root_group_indptr.assign(1, 0);
+  lay->root_group_req.clear();
+  lay->prompt_root.assign(size_t(R), -1);
+  std::vector<ps_choice> choice(size_t(R), ps_choice{});
+  for (int32_t r = 0; r < R; ++r) {
+    const int32_t p = base->req_prompt[size_t(r)], t = base->num_roots ? base->prompt_root[size_t(p)] : -1;
+    const int32_t seen = base->visible.empty() ? base->prefix_len[size_t(p)] : base->visible[size_t(r)];
+    const int32_t root_len = t >= 0 ? base->root_len[size_t(t)] : 0;
+    const int64_t num = ceil_div(root_len, B) + ceil_div(seen, B);
+    if (num > kPsSelectMostBlocks) return PS_ERR_UNSUPPORTED;
+    ps_choice& c = choice[size_t(r)];
+    c.request = r;
+    c.num_root = int32_t(ceil_div(root_len, B));
+    c.num = int32_t(num);
+    c.root_entry = t >= 0 ? root_blk0 + base->root_blk_indptr[size_t(t)] : 0;
+    c.prefix_entry = base->prefix_blk_indptr[size_t(p)];
+    c.skip = root_len % B ? c.num_root - 1 : -1;
+    c.first = std::min(opt.keep_first, c.num);
+    c.last = std::max(0, c.num - opt.keep_last);
+    const int32_t candidates = c.num - (c.skip >= 0), most = opt.blocks - (c.skip >= 0);
+    c.list = int32_t(lay->prefix_blk.size());
+    c.count = std::min(candidates, most);
+    // (position j of the context: which block)
+    auto block_at = [&](int32_t j) {
+      return j < c.num_root ? base->root_blk[size_t(base->root_blk_indptr[size_t(t)] + j)] : base->prefix_blk[size_t(c.prefix_entry + j - c.num_root)];
+    };
+    int32_t kept = 0;
+    c.open = candidates > most ? c.count : 0;
+    for (int32_t j = 0; j < c.num; ++j) {
+      if (j == c.skip) continue;
+      if (c.open > 0 && (j < c.first || j >= c.last) && candidates > most) --c.open;
+      // until the first choice: the beginning, and the last block in the last place, where its length counts
+      if (kept < c.count - 1 || (kept < c.count && j == c.num - 1) || (kept < c.count && c.skip == c.num - 1 && j == c.num - 2)) {
+        lay->prefix_blk.push_back(block_at(j));
+        ++kept;
+      }
+    }
+    lay->prefix_blk_indptr[size_t(r) + 1] = int32_t(lay->prefix_blk.size());
+    lay->prefix_len[size_t(r)] = c.count * B - (seen % B ? B - seen % B : 0);
+    if (c.skip >= 0) {
+      lay->prompt_root[size_t(r)] = lay->num_roots++;
+      lay->root_len.push_back(root_len % B);
+      lay->root_blk.push_back(block_at(c.skip));
+      lay->root_blk_indptr.push_back(int32_t(lay->root_blk.size()));
+      lay->root_group_req.push_back(r);
+      lay->root_group_indptr.push_back(int32_t(lay->root_group_req.size()));
+    }
+    if (candidates <= most) c.num = 0;   // nothing to choose
+  }
+  lay->head_stride = int64_t(lay->prefix_blk.size() + lay->suffix_blk.size() + lay->root_blk.size());
+  if (lay->head_stride * H > INT32_MAX) return PS_ERR_INVALID_ARG;
+  // The requests that choose, by prompt; the scoring work, a context range and up to 64 query rows of its prompt at a time.
+  ps_layout::selection& sel = *lay->sel;
+  const int32_t group = base->geo.num_q_heads / H;
+  int32_t columns = 1;   // of a request's query heads in the scoring products, padded
+  while (columns < std::min(group, 16)) columns *= 2;
+  if (group > 16) columns = (group + 15) / 16 * 16;
+  const int32_t per_item = std::max(1, 64 / columns);
+  std::vector<ps_choice> choices;
+  std::vector<ps_score_item> items;
+  int64_t score_words = 0;
+  sel.most_candidates = 0;
+  for (int32_t i = 0; i < R; ++i) {
+    ps_choice c = choice[size_t(base->group_req[size_t(i)])];
+    if (c.num == 0) continue;
+    c.scores = int32_t(score_words / 4);
+    score_words += int64_t(H) * round_up(c.num, 4);
+    if (score_words / 4 > INT32_MAX) return PS_ERR_INVALID_ARG;
+    sel.most_candidates = std::max(sel.most_candidates, c.num);
+    choices.push_back(c);
+  }
+  struct row_group { int32_t first, count, most; };   // of the choices, on one prompt
+  std::vector<row_group> groups;
+  int64_t blocks = 0;
+  for (size_t i = 0; i < choices.size(); i += size_t(groups.back().count)) {
+    row_group n{int32_t(i), 0, 0};
+    while (i + size_t(n.count) < choices.size() && n.count < per_item &&
+           base->req_prompt[size_t(choices[i + size_t(n.count)].request)] == base->req_prompt[size_t(choices[i].request)])
+      n.most = std::max(n.most, choices[i + size_t(n.count++)].num);
+    blocks += n.most;
+    groups.push_back(n);
+  }
+  // blocks an item takes: 64, a tile of 16 a wave, or what leaves four workgroups a compute unit
+  int32_t cus = ps_device_num_cus_hook ? ps_device_num_cus_hook() : 0;
+  if (cus <= 0) cus = kPsDefaultNumCus;
+  const int64_t chunk = std::max<int64_t>(64, round_up(ceil_div(blocks * H, 4 * int64_t(cus)), 64));
+  for (const row_group& n : groups) {
+    const ps_choice& c = choices[size_t(n.first)];   // (the prompt's requests share its context, and see more or less of it)
+    auto add = [&](int32_t entry, int32_t position, int32_t num) {
+      for (int64_t at = 0; at < num; at += chunk)
+        items.push_back({int32_t(entry + at), int32_t(position + at), int32_t(std::min<int64_t>(chunk, num - at)), n.first, n.count, {0, 0, 0}});
+    };
+    add(c.root_entry, 0, c.num_root);
+    add(c.prefix_entry, c.num_root, n.most - c.num_root);
+  }
+  sel.score_words = score_words;
+  auto words = [](const auto& from, std::vector<int32_t>& to) {
+    to.resize(from.size() * sizeof(from[0]) / 4);
+    if (!from.empty()) std::memcpy(to.data(), from.data(), to.size() * 4);
+  };
+  words(choices, sel.choices);
+  words(items, sel.score_items);
+  return PS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t ps_layout_select(const ps_layout* base, const ps_select_options* options, ps_layout** out) {
+  if (!base || !options || !out || base->parked || base->sel) return PS_ERR_INVALID_ARG;
+  const ps_geometry& g = base->geo;
+  if (options->keep_first < 0 || options->keep_last < 1 || options->blocks < 1 ||
+      int64_t(options->keep_first) + options->keep_last + (base->num_roots > 0) > options->blocks)
+    return PS_ERR_INVALID_ARG;
+  if (g.num_q_heads / g.num_kv_heads > kPsSelectMostGroup || (g.head_dim != 64 && g.head_dim != 128 && g.head_dim != 256))
+    return PS_ERR_UNSUPPORTED;
+  try {
+    std::unique_ptr<ps_layout> lay(new ps_layout());
+    lay->sel.reset(new ps_layout::selection());
+    lay->sel->opt = *options;
+    if (int32_t st = derive_selection(base, lay.get())) return st;
+    if (int32_t st = ps_plan_build(lay.get(), nullptr)) return st;
+    lay->sel->base_id = base->id;
+    lay->sel->base_version = base->version;
+    *out = lay.release();
+    return PS_OK;
+  } catch (const std::bad_alloc&) {
+    return PS_ERR_OOM;
+  }
+}
+
+int32_t ps_layout_select_follow(const ps_layout* base, ps_layout* lay) {
+  if (!base || !lay || !lay->sel || base->parked || lay->sel->base_id != base->id) return PS_ERR_INVALID_ARG;
+  lay->parked = true;   // (where it fails half-way nothing may be launched from it; the next follow mends it)
+  try {
+    const std::vector<int32_t> prefix_len = lay->prefix_len, root_len = lay->root_len, suffix_len = lay->suffix_len;
+    const std::vector<int32_t> prompt_root = lay->prompt_root;
+    const int64_t old_stride = lay->head_stride;
+    lay->sel->base_version = 0;
+    if (int32_t st = derive_selection(base, lay)) return st;
+    bool grown = prefix_len == lay->prefix_len && root_len == lay->root_len && prompt_root == lay->prompt_root;
+    for (size_t r = 0; r < suffix_len.size() && grown; ++r) grown = unsigned(lay->suffix_len[r] - suffix_len[r]) <= 1;
+    auto grew = [&](int32_t r) { return lay->suffix_len[size_t(r)] != suffix_len[size_t(r)]; };
+    if (int32_t st = grown ? plan_growth(lay, grew, old_stride) : ps_plan_build(lay, &lay->opt)) return st;
+  } catch (const std::bad_alloc&) {
+    return PS_ERR_OOM;
+  }
+  lay->sel->base_version = base->version;
+  lay->parked = false;
+  return PS_OK;
+}
+
+int32_t ps_select_lists(const ps_layout* lay, const int32_t** list_indptr, int64_t* head_stride) {
+  if (!lay || !lay->sel) return PS_ERR_INVALID_ARG;
+  if (list_indptr) *list_indptr = lay->prefix_blk_indptr.data();
+  if (head_stride) *head_stride = lay->head_stride;
+  return PS_OK;
+}
+
+int64_t ps_select_workspace_bytes(const ps_layout* lay) {
+  return lay && lay->sel ? std::max<int64_t>(16, lay->sel->score_words * 4) : -1;
+}
+
+int32_t ps_ingest_tokens(const ps_layout* lay, int32_t which, int64_t* out) {
+  if (!lay || !out || which < 0 || which > 2) return PS_ERR_INVALID_ARG;
+  const std::vector<int32_t>& len = which == 0 ? lay->prefix_len : which == 1 ? lay->suffix_len : lay->root_len;
+  int64_t n = 0;
+  for (int32_t l : len) n += l;
+  if (which == 0 && !lay->adopt_indptr.empty()) n -= int64_t(lay->adopt_indptr.back()) * lay->geo.block_size;
+  *out = n;
+  return PS_OK;
+}
+
+int32_t ps_rope_turns(int32_t count, const double* radians, uint64_t* out) {
+  if (count < 0 || (count && (!radians || !out))) return PS_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < count; ++i)
+    if (!(radians[i] >= 0.0) || std::isinf(radians[i])) return PS_ERR_INVALID_ARG;
+  for (int32_t i = 0; i < count; ++i) {
+    // (64 bits of significand where long double has them; a rate of a turn or more counts modulo a turn)
+    const long double turns = static_cast<long double>(radians[i]) / 6.283185307179586476925286766559005768L;
+    const long double fraction = turns - std::floor(turns);
+    const long double scaled = std::floor(fraction * 18446744073709551616.0L + 0.5L);
+    out[i] = scaled >= 18446744073709551616.0L ? 0 : static_cast<uint64_t>(scaled);
+  }
+  return PS_OK;
 }
 
 }  // extern "C"

@@ -1,10 +1,18 @@
 // Internal host-side structures shared by the layout/planner and the launch code.
 #pragma once
+#include <atomic>
 #include <cstdint>
 #include <deque>
+#include <memory>
 #include <vector>
 
 #include "prefillshare.h"
+
+// A number no other layout has.
+inline uint64_t ps_next_layout_id() {
+  static std::atomic<uint64_t> next{1};
+  return next.fetch_add(1, std::memory_order_relaxed);
+}
 
 struct ps_pool {
   int32_t num_blocks = 0;
@@ -29,6 +37,27 @@ struct ps_item {
 // bit 4: other items (further row groups of the same sharing group) read the same K/V range: keep it cacheable
 constexpr int32_t kPsItemSuffix = 1, kPsItemMasked = 2, kPsItemRowSplit = 4, kPsItemRoot = 8, kPsItemReread = 16;
 static_assert(sizeof(ps_item) == 32, "ps_item is 8 int32");
+
+// A request of a selection that has more candidates than it may take.  Positions count the blocks of its context, root first.
+struct ps_choice {
+  int32_t request;
+  int32_t root_entry, num_root;  // base's block array: the root's first entry, its blocks
+  int32_t prefix_entry;          // ... the prefix's
+  int32_t num;                   // positions: blocks of the root and of the visible prefix
+  int32_t list, count;           // the list's first word for KV head 0, and its length
+  int32_t scores;                // first score of KV head 0, in fours; (num + 3) / 4 of them per KV head
+  int32_t skip;                  // position of a partly filled last root block (a segment of its own), or -1
+  int32_t first, last;           // positions below first or from last on are always taken
+  int32_t open;                  // of the list, to be chosen by score
+};
+// One (context range, requests) of the scoring launch, all KV heads.
+struct ps_score_item {
+  int32_t entry, position, num;  // base's block array: first entry; its position in the context; blocks
+  int32_t choice, n_req;         // the requests: a range of the choices
+  int32_t unused[3];
+};
+static_assert(sizeof(ps_choice) == 48 && sizeof(ps_score_item) == 32, "read as int32 words");
+constexpr int32_t kPsSelectMostBlocks = 65536, kPsSelectMostGroup = 64;
 
 struct ps_layout {
   ps_geometry geo{};
@@ -111,6 +140,22 @@ struct ps_layout {
   std::vector<int32_t> ent_fixed_tok0, ent_fixed_valid;
   // ... and the order in which an ingest walks them: by physical block, within each kind
   std::vector<int32_t> ent_fixed_order;
+
+  // Which tables these are: a layout's own number, and one that rises whenever they are laid out anew.
+  uint64_t id = ps_next_layout_id(), version = 0;
+  // A selection (ps_layout_select): every request is a prompt of its own, whose prefix is the list of chosen blocks, per KV head:
+  // the block array is there once for every KV head, head_stride words apart, and the items' blk_off count that in.
+  struct selection {
+    ps_select_options opt{};
+    uint64_t base_id = 0, base_version = 0;
+    // 12 words per request that has to choose, by prompt (ps_choice), and 8 per unit of scoring work (ps_score_item)
+    std::vector<int32_t> choices, score_items;
+    int64_t off_choices = 0, off_score_items = 0;   // in the blob
+    int64_t score_words = 0;
+    int32_t most_candidates = 0;
+  };
+  std::unique_ptr<selection> sel;
+  int64_t head_stride = 0;
 
   // where the token of the most recent ps_layout_append went: block * B + slot per request, -1 = none
   std::vector<int32_t> append_dest;

@@ -37,6 +37,54 @@ def from_device(t: torch.Tensor) -> np.ndarray:
     return t.detach().to("cpu").to(torch.float64).numpy()
 
 
+class Rope:
+    """Norm and rotation of head rows: radians per position of every pair (float64, on the host), how elements pair up ("halves" or
+    "neighbours"), the norm's weights (device tensors [head_dim] in the rows' type, None = no norm) and epsilon."""
+
+    def __init__(self, radians, pairing="halves", q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
+                 eps: float = 1e-6, device="cuda:0"):
+        for w in (q_weight, k_weight):
+            if w is not None and not w.is_contiguous():
+                raise ValueError("norm weights are contiguous tensors")
+        turns = B.ps_rope_turns(radians)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device) if turns.size else None
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.struct = B.ps_rope(self.turns.data_ptr() if turns.size else 0, q_weight.data_ptr() if q_weight is not None else 0,
+                                k_weight.data_ptr() if k_weight is not None else 0, eps, 2 * turns.size, B.PAIRING.get(pairing, pairing))
+
+
+def _check_rows(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int | None, heads: int, dim: int):
+    if t.dim() != 3 or t.dtype != dtype or t.shape[1:] != (heads, dim) or (rows is not None and t.shape[0] != rows) or t.stride(2) != 1:
+        raise ValueError(f"{name}: rows [{'T' if rows is None else rows}, {heads}, {dim}] of {dtype} with contiguous elements are wanted")
+
+
+def _check_positions(t: torch.Tensor, rows: int):
+    if t.dtype != torch.int32 or t.shape != (rows,) or not t.is_contiguous():
+        raise ValueError(f"positions: a contiguous int32 tensor of {rows} is wanted")
+
+
+_TORCH_DTYPE = {B.PS_F32: torch.float32, B.PS_BF16: torch.bfloat16}
+
+
+def _stride(size: int, stride: int, least: int) -> int:
+    return stride if size > 1 else max(stride, least)   # (of an axis of one the stride is not used, and torch's may be anything)
+
+
+def rope_rows(geometry: B.ps_geometry, rope: Rope, src: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Queries of any number of tokens [T, Hq, d] normed and rotated; returns them contiguous (in `out` where given)."""
+    dtype = _TORCH_DTYPE[geometry.q_dtype]
+    _check_rows("src", src, dtype, None, geometry.num_q_heads, geometry.head_dim)
+    _check_positions(positions, src.shape[0])
+    if out is None:
+        out = torch.empty(src.shape, dtype=dtype, device=src.device)
+    elif out.shape != src.shape or out.dtype != dtype or not out.is_contiguous():
+        raise ValueError("out: a contiguous tensor like src is wanted")
+    d = geometry.head_dim
+    B.ps_rope_rows(geometry, rope.struct, src.shape[0], src.data_ptr(), _stride(src.shape[0], src.stride(0), d),
+                   _stride(src.shape[1], src.stride(1), d), positions.data_ptr(), out.data_ptr(), _stream())
+    return out
+
+
 class DecodeBatch:
     """Device-side state of one decode batch: uploaded tables, workspace, Q, output."""
 
@@ -118,6 +166,79 @@ class DecodeBatch:
         B.ps_kv_ingest(self.layout, self.tables.data_ptr(), which, src_k.data_ptr(), src_v.data_ptr(),
                        src_k.stride(0), src_k.stride(1), self.kv.data_ptr(), self._sc(), self._stream())
 
+    def kv_append_rope(self, rope: Rope, q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor):
+        """The tokens reserved by the last append, from raw projections [R, heads, d]: queries normed and rotated into self.q (q None:
+        left alone), keys normed and rotated and values into the cache."""
+        rows = self._token_rows(q, k, v, positions)
+        B.ps_kv_append_rope(self.layout, self.tables.data_ptr(), rope.struct, rows, self.q.data_ptr() if q is not None else 0,
+                            self.kv.data_ptr(), self._sc(), self._stream())
+
+    def _token_rows(self, q, k, v, positions):
+        g, n = self.geometry, self.num_requests
+        kv_dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
+        d = g.head_dim
+        for name, t, dtype, heads in (("q", q, _TORCH_DTYPE[g.q_dtype], g.num_q_heads), ("k", k, kv_dtype, g.num_kv_heads),
+                                      ("v", v, kv_dtype, g.num_kv_heads)):
+            if t is not None:
+                _check_rows(name, t, dtype, n, heads, d)
+        if k.stride() != v.stride():
+            raise ValueError("k and v have the same strides")
+        if q is not None and not self.q.is_contiguous():
+            raise ValueError("the batch's queries are a contiguous tensor")
+        _check_positions(positions, n)
+        return B.ps_token_rows(q.data_ptr() if q is not None else 0, k.data_ptr(), v.data_ptr(),
+                               _stride(n, q.stride(0), d) if q is not None else 0, _stride(g.num_q_heads, q.stride(1), d) if q is not None else 0,
+                               _stride(n, k.stride(0), d), _stride(g.num_kv_heads, k.stride(1), d), positions.data_ptr())
+
+    def kv_ingest_rope(self, which: int, rope: Rope, src_k: torch.Tensor, src_v: torch.Tensor, positions: torch.Tensor):
+        """kv_ingest of raw projections [T, Hkv, d]: keys normed and rotated on their way; positions int32 [T]."""
+        g = self.geometry
+        dtype, d = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16, g.head_dim
+        n = self._segment_tokens(which)
+        for name, t in (("src_k", src_k), ("src_v", src_v)):
+            _check_rows(name, t, dtype, n, g.num_kv_heads, d)
+        if src_v.stride() != src_k.stride():
+            raise ValueError("src_k and src_v have the same strides")
+        _check_positions(positions, n)
+        B.ps_kv_ingest_rope(self.layout, self.tables.data_ptr(), which, rope.struct, src_k.data_ptr(), src_v.data_ptr(),
+                            _stride(n, src_k.stride(0), d), _stride(g.num_kv_heads, src_k.stride(1), d), positions.data_ptr(),
+                            self.kv.data_ptr(), self._sc(), self._stream())
+
+    def kv_gather(self, which: int, dst_k: torch.Tensor, dst_v: torch.Tensor):
+        """The stored segments of one kind back into [T, Hkv, d] tensors, bf16 or float32 (kv_ingest the other way round)."""
+        g, d = self.geometry, self.geometry.head_dim
+        if dst_k.dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("dst_k, dst_v: bf16 or float32 tensors are wanted")
+        n = self._segment_tokens(which)
+        for name, t in (("dst_k", dst_k), ("dst_v", dst_v)):
+            _check_rows(name, t, dst_k.dtype, n, g.num_kv_heads, d)
+        if dst_v.stride() != dst_k.stride():
+            raise ValueError("dst_k and dst_v have the same strides")
+        B.ps_kv_gather(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(),
+                       B.PS_F32 if dst_k.dtype == torch.float32 else B.PS_BF16, dst_k.data_ptr(), dst_v.data_ptr(),
+                       _stride(n, dst_k.stride(0), d), _stride(g.num_kv_heads, dst_k.stride(1), d), self._stream())
+
+    def _segment_tokens(self, which: int) -> int:
+        """Tokens that an ingest of one kind of segment takes (adopted blocks aside)."""
+        return B.ps_ingest_tokens(self.layout, which)
+
+    def block_summaries(self, which: int, summaries: torch.Tensor, summary_scales: torch.Tensor):
+        """Eight-bit bounds of every block's keys: summaries int8 [num_blocks, Hkv, 2, d], summary_scales float32 [num_blocks, Hkv]."""
+        self._check_summaries(summaries, summary_scales)
+        B.ps_block_summaries(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(), summaries.data_ptr(),
+                             summary_scales.data_ptr(), self._stream())
+
+    def _check_summaries(self, summaries, summary_scales):
+        g = self.geometry
+        if (summaries.dtype != torch.int8 or summary_scales.dtype != torch.float32 or not summaries.is_contiguous() or
+                not summary_scales.is_contiguous() or summaries.shape != (summaries.shape[0], g.num_kv_heads, 2, g.head_dim) or
+                summary_scales.shape != summaries.shape[:2]):
+            raise ValueError("summaries: contiguous int8 [num_blocks, Hkv, 2, d] and float32 [num_blocks, Hkv] are wanted")
+
+    def select(self, blocks: int, keep_first: int = 1, keep_last: int = 2) -> "SelectedBatch":
+        """A step over `blocks` blocks of every request's shared context and its private tokens, chosen by the queries."""
+        return SelectedBatch(self, blocks, keep_first, keep_last)
+
     def append_step(self, pool, new_k: torch.Tensor, new_v: torch.Tensor, active=None):
         """One decode step of cache growth: tables grow on the host and are uploaded again, then the new
         tokens ([R, Hkv, d], contiguous) are stored.  Returns the destinations the host chose."""
@@ -155,3 +276,49 @@ class DecodeBatch:
         o = self.workspace[:off].view(torch.float32).view(slots, g.num_q_heads, g.head_dim)
         lse = self.workspace[off:off + slots * g.num_q_heads * 4].view(torch.float32).view(slots, g.num_q_heads)
         return o, lse
+
+
+class SelectedBatch(DecodeBatch):
+    """A selection over a DecodeBatch: its queries and cache, block lists of its own.  select_blocks() chooses, decode_attention() and
+    its parts attend; after append_step, set_visible or replan of the base, follow()."""
+
+    def __init__(self, base: DecodeBatch, blocks: int, keep_first: int = 1, keep_last: int = 2):
+        self.base, self.scratch, self._lists = base, None, None
+        layout = B.ps_layout_select(base.layout, blocks, keep_first, keep_last)
+        super().__init__(layout, base.geometry, base.num_requests, base.q, base.kv, base.scales)
+
+    def _sync_plan(self, wait=True, tokens=None):
+        super()._sync_plan(wait, tokens)
+        self.scratch = torch.empty(B.ps_select_workspace_bytes(self.layout), dtype=torch.uint8, device=self.device)
+        indptr, stride = B.ps_select_lists(self.layout, self.num_requests)
+        self._lists = self.tables.view(torch.int32).as_strided((self.geometry.num_kv_heads, int(indptr[-1])), (stride, 1))
+
+    def _stream(self) -> int:
+        stream = super()._stream()
+        if stream != self._home:
+            self.scratch.record_stream(torch.cuda.current_stream())
+        return stream
+
+    def select_blocks(self, summaries: torch.Tensor, summary_scales: torch.Tensor):
+        """Scores every block of the shared contexts against the base's queries and writes the lists of the highest."""
+        self._check_summaries(summaries, summary_scales)
+        base = self.base
+        self.q = base.q
+        tables = base.tables.data_ptr()
+        base._stream()                       # (the base's tables, too, behind their upload)
+        B.ps_select_blocks(base.layout, tables, self.layout, self.tables.data_ptr(), self.q.data_ptr(), summaries.data_ptr(),
+                           summary_scales.data_ptr(), self.scratch.data_ptr(), self._stream())
+
+    def follow(self):
+        """In line with the base again.  Like the base's append_step it does not wait on the host."""
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("follow changes the tables on the host: it cannot be recorded into a graph")
+        B.ps_layout_select_follow(self.base.layout, self.layout)
+        self._sync_plan(wait=False)
+
+    def lists(self) -> torch.Tensor:
+        """The chosen blocks, int32 [Hkv, sum of the list lengths] (requests one behind another, see list_indptr()): a view."""
+        return self._lists
+
+    def list_indptr(self) -> np.ndarray:
+        return B.ps_select_lists(self.layout, self.num_requests)[0]
