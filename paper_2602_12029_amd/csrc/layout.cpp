@@ -1723,24 +1723,18 @@ int32_t derive_selection(const ps_layout* base, ps_layout* lay) {
   }
   struct row_group { int32_t first, count, most; };   // of the choices, on one prompt
   std::vector<row_group> groups;
-  int64_t blocks = 0;
   for (size_t i = 0; i < choices.size(); i += size_t(groups.back().count)) {
     row_group n{int32_t(i), 0, 0};
     while (i + size_t(n.count) < choices.size() && n.count < per_item &&
            base->req_prompt[size_t(choices[i + size_t(n.count)].request)] == base->req_prompt[size_t(choices[i].request)])
       n.most = std::max(n.most, choices[i + size_t(n.count++)].num);
-    blocks += n.most;
     groups.push_back(n);
   }
-  // blocks an item takes: 64, a tile of 16 a wave, or what leaves four workgroups a compute unit
-  int32_t cus = ps_device_num_cus_hook ? ps_device_num_cus_hook() : 0;
-  if (cus <= 0) cus = kPsDefaultNumCus;
-  const int64_t chunk = std::max<int64_t>(64, round_up(ceil_div(blocks * H, 4 * int64_t(cus)), 64));
   for (const row_group& n : groups) {
     const ps_choice& c = choices[size_t(n.first)];   // (the prompt's requests share its context, and see more or less of it)
     auto add = [&](int32_t entry, int32_t position, int32_t num) {
-      for (int64_t at = 0; at < num; at += chunk)
-        items.push_back({int32_t(entry + at), int32_t(position + at), int32_t(std::min<int64_t>(chunk, num - at)), n.first, n.count, {0, 0, 0}});
+      for (int32_t at = 0; at < num; at += kPsScoreBlocks)
+        items.push_back({entry + at, position + at, std::min(kPsScoreBlocks, num - at), n.first, n.count, {0, 0, 0}});
     };
     add(c.root_entry, 0, c.num_root);
     add(c.prefix_entry, c.num_root, n.most - c.num_root);

@@ -58,6 +58,7 @@ struct ps_score_item {
 };
 static_assert(sizeof(ps_choice) == 48 && sizeof(ps_score_item) == 32, "read as int32 words");
 constexpr int32_t kPsSelectMostBlocks = 65536, kPsSelectMostGroup = 64;
+constexpr int32_t kPsScoreBlocks = 128;   // blocks that a workgroup of the scoring launch takes in a round
 
 struct ps_layout {
   ps_geometry geo{};

@@ -185,7 +185,7 @@ def test_equal_scores_and_odd_queries(gpu):
     case.close()
 
 
-@pytest.mark.parametrize("blocks_of", [900, 1500, 3001, 5000, 8192, 8193, 20011])
+@pytest.mark.parametrize("blocks_of", [900, 1500, 2049, 3001, 5000, 8192, 8193, 16384, 16385, 20011])
 def test_long_contexts(gpu, blocks_of):
     """Every size of the choice kernel, scores with many equal ones and wide ranges; the lists alone."""
     from paper_2602_12029_amd import binding as B
