@@ -117,8 +117,15 @@ def _lib():
                                 "ps_prefix_suffix_attention": 7, "ps_merge_states": 6, "ps_decode_attention": 9,
                                 "ps_decode_attention_static": 8, "ps_kv_append": 7, "ps_layout_upload_append": 7}.items():
                 getattr(lib, name).argtypes = [C.c_void_p] + [C.c_size_t] * (count - 1)
-            lib.ps_kv_append_rope.argtypes = [C.c_void_p, C.c_size_t, C.POINTER(ps_rope), C.POINTER(ps_token_rows)] + [C.c_size_t] * 4
-            lib.ps_select_blocks.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p] + [C.c_size_t] * 6
+            A, I, S = C.c_size_t, C.c_int32, C.c_int64     # an address, a number, a stride
+            rope = C.POINTER(ps_rope)
+            for name, args in {"ps_rope_rows": [C.POINTER(ps_geometry), rope, S, A, S, S, A, A, A],
+                               "ps_kv_append_rope": [C.c_void_p, A, rope, C.POINTER(ps_token_rows), A, A, A, A],
+                               "ps_kv_ingest_rope": [C.c_void_p, A, I, rope, A, A, S, S, A, A, A, A],
+                               "ps_kv_gather": [C.c_void_p, A, I, A, A, I, A, A, S, S, A],
+                               "ps_block_summaries": [C.c_void_p, A, I, A, A, A, A, A],
+                               "ps_select_blocks": [C.c_void_p, A, C.c_void_p, A, A, A, A, A, A]}.items():
+                getattr(lib, name).argtypes = args
         for name in EXPORTS:
             if not (host_only and name in DEVICE_EXPORTS):
                 getattr(lib, name)                  # fail early if a symbol is missing
@@ -455,6 +462,7 @@ def ps_probe_read(dev_buf, nbytes: int, pattern: int, num_workgroups: int, strea
 
 
 # ---- norm, rotation and cache write in one pass; reading back ----------------------------------------
+# (addresses are integers, 0 = NULL: declared with the library, ctypes converts and checks them)
 def ps_rope_turns(radians) -> np.ndarray:
     """Rates as 64-bit fractions of a turn per position."""
     rad = np.ascontiguousarray(radians, dtype=np.float64)
@@ -465,28 +473,23 @@ def ps_rope_turns(radians) -> np.ndarray:
 
 
 def ps_rope_rows(geo: ps_geometry, rope: ps_rope, num_rows: int, src, src_stride_row: int, src_stride_head: int, positions, out, stream=0):
-    _check(_lib().ps_rope_rows(C.byref(geo), C.byref(rope), C.c_int64(num_rows), _p(src), C.c_int64(src_stride_row),
-                               C.c_int64(src_stride_head), _p(positions), _p(out), _p(stream)), "ps_rope_rows")
+    _check(_lib().ps_rope_rows(geo, rope, num_rows, src, src_stride_row, src_stride_head, positions, out, stream), "ps_rope_rows")
 
 
 def ps_kv_append_rope(layout, dev_tables, rope: ps_rope, rows: ps_token_rows, q_out, kv_pool, kv_scales, stream=0):
-    status = _lib().ps_kv_append_rope(layout, int(dev_tables or 0), rope, rows, int(q_out or 0), int(kv_pool or 0), int(kv_scales or 0),
-                                      int(stream or 0))
-    if status != PS_OK:
-        raise PsError(status, "ps_kv_append_rope")
+    _check(_lib().ps_kv_append_rope(layout, dev_tables, rope, rows, q_out, kv_pool, kv_scales, stream), "ps_kv_append_rope")
 
 
 def ps_kv_ingest_rope(layout, dev_tables, which: int, rope: ps_rope, src_k, src_v, src_stride_tok: int, src_stride_head: int, positions,
                       kv_pool, kv_scales, stream=0):
-    _check(_lib().ps_kv_ingest_rope(layout, _p(dev_tables), C.c_int32(which), C.byref(rope), _p(src_k), _p(src_v),
-                                    C.c_int64(src_stride_tok), C.c_int64(src_stride_head), _p(positions), _p(kv_pool), _p(kv_scales),
-                                    _p(stream)), "ps_kv_ingest_rope")
+    _check(_lib().ps_kv_ingest_rope(layout, dev_tables, which, rope, src_k, src_v, src_stride_tok, src_stride_head, positions, kv_pool,
+                                    kv_scales, stream), "ps_kv_ingest_rope")
 
 
 def ps_kv_gather(layout, dev_tables, which: int, kv_pool, kv_scales, dst_dtype: int, dst_k, dst_v, dst_stride_tok: int,
                  dst_stride_head: int, stream=0):
-    _check(_lib().ps_kv_gather(layout, _p(dev_tables), C.c_int32(which), _p(kv_pool), _p(kv_scales), C.c_int32(dst_dtype), _p(dst_k),
-                               _p(dst_v), C.c_int64(dst_stride_tok), C.c_int64(dst_stride_head), _p(stream)), "ps_kv_gather")
+    _check(_lib().ps_kv_gather(layout, dev_tables, which, kv_pool, kv_scales, dst_dtype, dst_k, dst_v, dst_stride_tok, dst_stride_head,
+                               stream), "ps_kv_gather")
 
 
 def ps_ingest_tokens(layout, which: int) -> int:
@@ -497,8 +500,7 @@ def ps_ingest_tokens(layout, which: int) -> int:
 
 # ---- a step over chosen blocks -------------------------------------------------------------------------
 def ps_block_summaries(layout, dev_tables, which: int, kv_pool, kv_scales, summaries, summary_scales, stream=0):
-    _check(_lib().ps_block_summaries(layout, _p(dev_tables), C.c_int32(which), _p(kv_pool), _p(kv_scales), _p(summaries),
-                                     _p(summary_scales), _p(stream)), "ps_block_summaries")
+    _check(_lib().ps_block_summaries(layout, dev_tables, which, kv_pool, kv_scales, summaries, summary_scales, stream), "ps_block_summaries")
 
 
 def ps_layout_select(layout, blocks: int, keep_first: int = 1, keep_last: int = 2):
@@ -524,10 +526,8 @@ def ps_select_workspace_bytes(selection) -> int:
 
 
 def ps_select_blocks(layout, dev_tables, selection, selection_tables, q, summaries, summary_scales, workspace, stream=0):
-    status = _lib().ps_select_blocks(layout, int(dev_tables or 0), selection, int(selection_tables or 0), int(q or 0), int(summaries or 0),
-                                     int(summary_scales or 0), int(workspace or 0), int(stream or 0))
-    if status != PS_OK:
-        raise PsError(status, "ps_select_blocks")
+    _check(_lib().ps_select_blocks(layout, dev_tables, selection, selection_tables, q, summaries, summary_scales, workspace, stream),
+           "ps_select_blocks")
 
 
 def ps_layout_park(pool, layout):

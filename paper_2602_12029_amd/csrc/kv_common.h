@@ -33,6 +33,45 @@ __device__ __forceinline__ float wave_max(float x) {
   return x;
 }
 
+// x of another lane by a DPP control; lanes without one (and rows of 16 outside `ROWS`) get `none`
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t none, uint32_t x) {
+  return uint32_t(__builtin_amdgcn_update_dpp(int(none), int(x), CTRL, ROWS, 0xf, false));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kRor8 = 0x128, kBcast15 = 0x142, kBcast31 = 0x143;
+
+constexpr float kMost = 0x1.fffffep127f;   // the largest finite float32
+
+// Eight-bit rows (block summaries, query rows that meet them): the scale of rows whose largest magnitude is `top`, and the codes,
+// round to nearest even of x / scale, four to a word, of finite x of a whole wavefront.
+// x / scale without a division per element: x times the instruction's reciprocal (one step off) is within 2^-15 of it (|x / scale|
+// < 128), and adding 1.5 * 2^23 rounds to nearest even in place, the code in the low byte; where any of a wave's quotients lies within
+// 2^-14 of half a step, the real division decides.
+__device__ __forceinline__ float eight_bit_scale(float top) {
+  const float scale = top * (1.f / 127.f);
+  return scale >= 0x1p-126f ? scale : 1.f;
+}
+template <int N>
+__device__ __forceinline__ void eight_bit_codes(const float (&x)[N], float scale, uint32_t (&codes)[N / 4]) {
+  constexpr float kMagic = 12582912.f;
+  const float rinv = __builtin_amdgcn_rcpf(scale);
+  uint32_t byte[N];
+  float off = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float y = __builtin_fmaf(x[j], rinv, kMagic);
+    byte[j] = __float_as_uint(y);
+    off = fmaxf(off, fabsf(__builtin_fmaf(x[j], rinv, kMagic - y)));
+  }
+  if (__builtin_amdgcn_ballot_w64(off > 0.5f - 0x1p-14f) != 0) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) byte[j] = __float_as_uint(x[j] / scale + kMagic);
+  }
+#pragma unroll
+  for (int j = 0; j < N; j += 4)
+    codes[j / 4] = __builtin_amdgcn_perm(byte[j + 1], byte[j], 0x0c0c0400u) | __builtin_amdgcn_perm(byte[j + 3], byte[j + 2], 0x04000c0cu);
+}
+
 struct KvWriteParams {
   const int32_t* blk;        // concatenated block array
   const int32_t* ent_tok0;   // per entry: its first token in the ragged source of its kind

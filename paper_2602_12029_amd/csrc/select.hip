@@ -35,13 +35,9 @@ struct SelectParams {
 };
 
 constexpr int kRows = 64;              // query rows of an item, padded
-constexpr float kMost = 0x1.fffffep127f;
 
-// Codes of eight-bit rows: x[N] of 16 lanes to a row, each to the byte of round to nearest even of x / scale, four to a word, and
-// the row's scale.  x / scale without a division per element: x * RN(1 / scale) is within 2^-15 of it (|x / scale| < 128), and
-// adding 1.5 * 2^23 rounds to nearest even in place, the code in the low byte; where any of a wave's quotients lies within
-// 2^-14 of half a step, the real division decides.  The largest magnitude is an integer maximum of the bits, which also shows
-// what is not finite: counted as 0 (no number) or the largest finite one.
+// Codes of a query row, x[N] of 16 lanes each, four to a word, and its scale.  The largest magnitude is an integer maximum of
+// the bits, which also shows what is not finite: counted as 0 (no number) or the largest finite one.
 template <int N>
 __device__ __forceinline__ float row16_codes(float (&x)[N], uint32_t (&codes)[N / 4]) {
   constexpr uint32_t kMagnitude = 0x7fffffffu, kMostBits = 0x7f7fffffu;
@@ -56,31 +52,12 @@ __device__ __forceinline__ float row16_codes(float (&x)[N], uint32_t (&codes)[N 
       top = max(top, __float_as_uint(x[j]) & kMagnitude);
     }
   }
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0xB1, 0xf, 0xf, true)));
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x4E, 0xf, 0xf, true)));
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x141, 0xf, 0xf, true)));
-  top = max(top, uint32_t(__builtin_amdgcn_update_dpp(0, int(top), 0x140, 0xf, 0xf, true)));
-  float scale = __uint_as_float(top) * (1.f / 127.f);
-  if (!(scale >= 0x1p-126f)) scale = 1.f;
-  constexpr float kMagic = 12582912.f;
-  const float rinv = 1.f / scale;
-  uint32_t byte[N];
-  float off = 0.f;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float y = __builtin_fmaf(x[j], rinv, kMagic);
-    byte[j] = __float_as_uint(y);
-    off = fmaxf(off, fabsf(__builtin_fmaf(x[j], rinv, kMagic - y)));
-  }
-  if (__builtin_amdgcn_ballot_w64(off > 0.5f - 0x1p-14f) != 0) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) byte[j] = __float_as_uint(x[j] / scale + kMagic);
-  }
-#pragma unroll
-  for (int j = 0; j < N; j += 4) {
-    const uint32_t low = __builtin_amdgcn_perm(byte[j + 1], byte[j], 0x0c0c0400u), high = __builtin_amdgcn_perm(byte[j + 3], byte[j + 2], 0x04000c0cu);
-    codes[j / 4] = low | high;
-  }
+  top = max(top, dpp_u32<kXor1>(0, top));
+  top = max(top, dpp_u32<kXor2>(0, top));
+  top = max(top, dpp_u32<kHalfMirror>(0, top));
+  top = max(top, dpp_u32<kMirror>(0, top));
+  const float scale = eight_bit_scale(__uint_as_float(top));
+  eight_bit_codes<N>(x, scale, codes);
   return scale;
 }
 
@@ -233,42 +210,36 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t order) { return __uint_as_float((order >> 31) ? order ^ 0x80000000u : ~order); }
 
-// x of another lane by a DPP control; lanes without one (and rows outside `rows`) get `none`
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ uint32_t dpp(uint32_t none, uint32_t x) {
-  return uint32_t(__builtin_amdgcn_update_dpp(int(none), int(x), CTRL, ROWS, 0xf, false));
-}
-constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140, kBcast15 = 0x142, kBcast31 = 0x143;
 // over the wave, uniform
 __device__ __forceinline__ uint32_t wave_min_u32(uint32_t x) {
-  x = min(x, dpp<kXor1>(x, x));
-  x = min(x, dpp<kXor2>(x, x));
-  x = min(x, dpp<kHalfMirror>(x, x));
-  x = min(x, dpp<kMirror>(x, x));
-  x = min(x, dpp<kBcast15, 0xa>(x, x));
-  x = min(x, dpp<kBcast31, 0xc>(x, x));
+  x = min(x, dpp_u32<kXor1>(x, x));
+  x = min(x, dpp_u32<kXor2>(x, x));
+  x = min(x, dpp_u32<kHalfMirror>(x, x));
+  x = min(x, dpp_u32<kMirror>(x, x));
+  x = min(x, dpp_u32<kBcast15, 0xa>(x, x));
+  x = min(x, dpp_u32<kBcast31, 0xc>(x, x));
   return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
 }
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) { return ~wave_min_u32(~x); }
 // over 4 or 16 neighbouring lanes
 template <int N>
 __device__ __forceinline__ uint32_t few_min_u32(uint32_t x) {
-  x = min(x, dpp<kXor1>(x, x));
-  x = min(x, dpp<kXor2>(x, x));
+  x = min(x, dpp_u32<kXor1>(x, x));
+  x = min(x, dpp_u32<kXor2>(x, x));
   if constexpr (N == 16) {
-    x = min(x, dpp<kHalfMirror>(x, x));
-    x = min(x, dpp<kMirror>(x, x));
+    x = min(x, dpp_u32<kHalfMirror>(x, x));
+    x = min(x, dpp_u32<kMirror>(x, x));
   }
   return uint32_t(__builtin_amdgcn_readfirstlane(int(x)));
 }
 // sum of the lanes up to and with this one
 __device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
-  x += dpp<0x111>(0, x);   // row_shr 1, 2, 4, 8
-  x += dpp<0x112>(0, x);
-  x += dpp<0x114>(0, x);
-  x += dpp<0x118>(0, x);
-  x += dpp<kBcast15, 0xa>(0, x);
-  x += dpp<kBcast31, 0xc>(0, x);
+  x += dpp_u32<0x111>(0, x);   // row_shr 1, 2, 4, 8
+  x += dpp_u32<0x112>(0, x);
+  x += dpp_u32<0x114>(0, x);
+  x += dpp_u32<0x118>(0, x);
+  x += dpp_u32<kBcast15, 0xa>(0, x);
+  x += dpp_u32<kBcast31, 0xc>(0, x);
   return x;
 }
 

@@ -53,35 +53,33 @@ class Rope:
                                 k_weight.data_ptr() if k_weight is not None else 0, eps, 2 * turns.size, B.PAIRING.get(pairing, pairing))
 
 
-def _check_rows(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int | None, heads: int, dim: int):
-    if t.dim() != 3 or t.dtype != dtype or t.shape[1:] != (heads, dim) or (rows is not None and t.shape[0] != rows) or t.stride(2) != 1:
-        raise ValueError(f"{name}: rows [{'T' if rows is None else rows}, {heads}, {dim}] of {dtype} with contiguous elements are wanted")
+def _row_strides(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, dim: int):
+    """(row, head) strides of rows [rows, heads, dim] with contiguous elements; anything else is refused."""
+    strides = t.stride()
+    if t.dtype is not dtype or t.shape != (rows, heads, dim) or strides[2] != 1:
+        raise ValueError(f"{name}: rows [{rows}, {heads}, {dim}] of {dtype} with contiguous elements are wanted")
+    # (of an axis of one the stride is not used, and torch's may be anything)
+    return strides[0] if rows > 1 else max(strides[0], dim), strides[1] if heads > 1 else max(strides[1], dim)
 
 
 def _check_positions(t: torch.Tensor, rows: int):
-    if t.dtype != torch.int32 or t.shape != (rows,) or not t.is_contiguous():
+    if t.dtype is not torch.int32 or t.shape != (rows,) or (rows > 1 and t.stride(0) != 1):
         raise ValueError(f"positions: a contiguous int32 tensor of {rows} is wanted")
 
 
 _TORCH_DTYPE = {B.PS_F32: torch.float32, B.PS_BF16: torch.bfloat16}
 
 
-def _stride(size: int, stride: int, least: int) -> int:
-    return stride if size > 1 else max(stride, least)   # (of an axis of one the stride is not used, and torch's may be anything)
-
-
 def rope_rows(geometry: B.ps_geometry, rope: Rope, src: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """Queries of any number of tokens [T, Hq, d] normed and rotated; returns them contiguous (in `out` where given)."""
-    dtype = _TORCH_DTYPE[geometry.q_dtype]
-    _check_rows("src", src, dtype, None, geometry.num_q_heads, geometry.head_dim)
-    _check_positions(positions, src.shape[0])
+    dtype, n = _TORCH_DTYPE[geometry.q_dtype], src.shape[0]
+    row, head = _row_strides("src", src, dtype, n, geometry.num_q_heads, geometry.head_dim)
+    _check_positions(positions, n)
     if out is None:
         out = torch.empty(src.shape, dtype=dtype, device=src.device)
-    elif out.shape != src.shape or out.dtype != dtype or not out.is_contiguous():
+    elif out.shape != src.shape or out.dtype is not dtype or not out.is_contiguous():
         raise ValueError("out: a contiguous tensor like src is wanted")
-    d = geometry.head_dim
-    B.ps_rope_rows(geometry, rope.struct, src.shape[0], src.data_ptr(), _stride(src.shape[0], src.stride(0), d),
-                   _stride(src.shape[1], src.stride(1), d), positions.data_ptr(), out.data_ptr(), _stream())
+    B.ps_rope_rows(geometry, rope.struct, n, src.data_ptr(), row, head, positions.data_ptr(), out.data_ptr(), _stream())
     return out
 
 
@@ -175,48 +173,42 @@ class DecodeBatch:
 
     def _token_rows(self, q, k, v, positions):
         g, n = self.geometry, self.num_requests
-        kv_dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
-        d = g.head_dim
-        for name, t, dtype, heads in (("q", q, _TORCH_DTYPE[g.q_dtype], g.num_q_heads), ("k", k, kv_dtype, g.num_kv_heads),
-                                      ("v", v, kv_dtype, g.num_kv_heads)):
-            if t is not None:
-                _check_rows(name, t, dtype, n, heads, d)
-        if k.stride() != v.stride():
+        heads, d = g.num_kv_heads, g.head_dim
+        dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
+        strides = _row_strides("k", k, dtype, n, heads, d)
+        if _row_strides("v", v, dtype, n, heads, d) != strides:
             raise ValueError("k and v have the same strides")
-        if q is not None and not self.q.is_contiguous():
-            raise ValueError("the batch's queries are a contiguous tensor")
         _check_positions(positions, n)
-        return B.ps_token_rows(q.data_ptr() if q is not None else 0, k.data_ptr(), v.data_ptr(),
-                               _stride(n, q.stride(0), d) if q is not None else 0, _stride(g.num_q_heads, q.stride(1), d) if q is not None else 0,
-                               _stride(n, k.stride(0), d), _stride(g.num_kv_heads, k.stride(1), d), positions.data_ptr())
+        if q is None:
+            return B.ps_token_rows(0, k.data_ptr(), v.data_ptr(), 0, 0, *strides, positions.data_ptr())
+        q_strides = _row_strides("q", q, _TORCH_DTYPE[g.q_dtype], n, g.num_q_heads, d)
+        if not self.q.is_contiguous():
+            raise ValueError("the batch's queries are a contiguous tensor")
+        return B.ps_token_rows(q.data_ptr(), k.data_ptr(), v.data_ptr(), *q_strides, *strides, positions.data_ptr())
 
     def kv_ingest_rope(self, which: int, rope: Rope, src_k: torch.Tensor, src_v: torch.Tensor, positions: torch.Tensor):
         """kv_ingest of raw projections [T, Hkv, d]: keys normed and rotated on their way; positions int32 [T]."""
-        g = self.geometry
-        dtype, d = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16, g.head_dim
-        n = self._segment_tokens(which)
-        for name, t in (("src_k", src_k), ("src_v", src_v)):
-            _check_rows(name, t, dtype, n, g.num_kv_heads, d)
-        if src_v.stride() != src_k.stride():
+        g, n = self.geometry, self._segment_tokens(which)
+        heads, d = g.num_kv_heads, g.head_dim
+        dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
+        strides = _row_strides("src_k", src_k, dtype, n, heads, d)
+        if _row_strides("src_v", src_v, dtype, n, heads, d) != strides:
             raise ValueError("src_k and src_v have the same strides")
         _check_positions(positions, n)
-        B.ps_kv_ingest_rope(self.layout, self.tables.data_ptr(), which, rope.struct, src_k.data_ptr(), src_v.data_ptr(),
-                            _stride(n, src_k.stride(0), d), _stride(g.num_kv_heads, src_k.stride(1), d), positions.data_ptr(),
-                            self.kv.data_ptr(), self._sc(), self._stream())
+        B.ps_kv_ingest_rope(self.layout, self.tables.data_ptr(), which, rope.struct, src_k.data_ptr(), src_v.data_ptr(), *strides,
+                            positions.data_ptr(), self.kv.data_ptr(), self._sc(), self._stream())
 
     def kv_gather(self, which: int, dst_k: torch.Tensor, dst_v: torch.Tensor):
         """The stored segments of one kind back into [T, Hkv, d] tensors, bf16 or float32 (kv_ingest the other way round)."""
-        g, d = self.geometry, self.geometry.head_dim
-        if dst_k.dtype not in (torch.bfloat16, torch.float32):
+        g, n, dtype = self.geometry, self._segment_tokens(which), dst_k.dtype
+        heads, d = g.num_kv_heads, g.head_dim
+        if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise ValueError("dst_k, dst_v: bf16 or float32 tensors are wanted")
-        n = self._segment_tokens(which)
-        for name, t in (("dst_k", dst_k), ("dst_v", dst_v)):
-            _check_rows(name, t, dst_k.dtype, n, g.num_kv_heads, d)
-        if dst_v.stride() != dst_k.stride():
+        strides = _row_strides("dst_k", dst_k, dtype, n, heads, d)
+        if _row_strides("dst_v", dst_v, dtype, n, heads, d) != strides:
             raise ValueError("dst_k and dst_v have the same strides")
         B.ps_kv_gather(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(),
-                       B.PS_F32 if dst_k.dtype == torch.float32 else B.PS_BF16, dst_k.data_ptr(), dst_v.data_ptr(),
-                       _stride(n, dst_k.stride(0), d), _stride(g.num_kv_heads, dst_k.stride(1), d), self._stream())
+                       B.PS_F32 if dtype is torch.float32 else B.PS_BF16, dst_k.data_ptr(), dst_v.data_ptr(), *strides, self._stream())
 
     def _segment_tokens(self, which: int) -> int:
         """Tokens that an ingest of one kind of segment takes (adopted blocks aside)."""
@@ -229,10 +221,9 @@ class DecodeBatch:
                              summary_scales.data_ptr(), self._stream())
 
     def _check_summaries(self, summaries, summary_scales):
-        g = self.geometry
-        if (summaries.dtype != torch.int8 or summary_scales.dtype != torch.float32 or not summaries.is_contiguous() or
-                not summary_scales.is_contiguous() or summaries.shape != (summaries.shape[0], g.num_kv_heads, 2, g.head_dim) or
-                summary_scales.shape != summaries.shape[:2]):
+        heads, n = self.geometry.num_kv_heads, summaries.shape[0]
+        if (summaries.dtype is not torch.int8 or summary_scales.dtype is not torch.float32 or summaries.shape != (n, heads, 2, self.geometry.head_dim) or
+                summary_scales.shape != (n, heads) or not summaries.is_contiguous() or not summary_scales.is_contiguous()):
             raise ValueError("summaries: contiguous int8 [num_blocks, Hkv, 2, d] and float32 [num_blocks, Hkv] are wanted")
 
     def select(self, blocks: int, keep_first: int = 1, keep_last: int = 2) -> "SelectedBatch":
@@ -304,9 +295,8 @@ class SelectedBatch(DecodeBatch):
         self._check_summaries(summaries, summary_scales)
         base = self.base
         self.q = base.q
-        tables = base.tables.data_ptr()
         base._stream()                       # (the base's tables, too, behind their upload)
-        B.ps_select_blocks(base.layout, tables, self.layout, self.tables.data_ptr(), self.q.data_ptr(), summaries.data_ptr(),
+        B.ps_select_blocks(base.layout, base.tables.data_ptr(), self.layout, self.tables.data_ptr(), base.q.data_ptr(), summaries.data_ptr(),
                            summary_scales.data_ptr(), self.scratch.data_ptr(), self._stream())
 
     def follow(self):
