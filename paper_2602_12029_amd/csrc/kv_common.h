@@ -84,44 +84,27 @@ struct KvWriteParams {
   int64_t s_block, s_head, s_kv, s_tok;  // pool strides, elements
 };
 
-// Codes of x / scale, round to nearest even, for eight values a lane of a whole wavefront (`live`: this lane's count).
-// x / scale without a division per element.  q0 = x * RN(1 / scale) is within 2 ulp of the exact quotient and
-// the correctly rounded quotient within 0.5 ulp, so both lie on the same side of every rounding boundary of
-// e4m3 -- and get the same code -- unless q0 is within a few ulp of one.  Boundaries (midpoints of neighbouring
-// e4m3 values) have the float32 pattern "3 mantissa bits, then 1000...0" in the normal range; a piece in which
-// any lane is that close to one, or may fall into the subnormal range of e4m3 (an absolute grid), is redone with
-// the real division.  The stored codes are therefore exactly those of RN(x / scale) everywhere.
+// Codes of x / scale, round to nearest even, for eight values a lane: exactly those of the correctly rounded float32 quotient,
+// without a division per element.  With y the correctly rounded 1 / scale, q = x y is within two steps of the quotient; a
+// correction q <- q - (q scale - x) y brings it within one, and by Markstein's theorem (IBM J. Res. Dev. 34, 1990: y correctly
+// rounded, q within one step, the residual exact) the next one to the correctly rounded quotient.  The residual is written with
+// this sign so that -0 keeps its own.  The residuals are exact where they do not underflow: from 2^-10 of the scale on, below
+// which the code is 0 either way, so for any scale from 2^-90; the others, and infinities, are divided.
 struct E4m3Encoder {
-  float scale, rinv, subnormal_below;
-  __device__ __forceinline__ explicit E4m3Encoder(float s)
-      // |x| under this: the quotient may be under 2^-6 (and any |x| where the reciprocal overflows)
-      : scale(s), rinv(1.f / s), subnormal_below(s < 0x1p-126f ? __builtin_inff() : s * 0x1.000002p-6f) {}
-  __device__ __forceinline__ u32x2 operator()(const float (&x)[8], bool live) const {
+  float scale, rinv;
+  bool divide;   // uniform
+  __device__ __forceinline__ explicit E4m3Encoder(float s) : scale(s), rinv(1.f / s), divide(!(s >= 0x1p-90f && s <= 0x1p120f)) {}
+  __device__ __forceinline__ u32x2 operator()(const float (&x)[8]) const {
     float q[8];
-    bool risky = false;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       q[j] = x[j] * rinv;
-      // low 20 mantissa bits within [0x7fffc, 0x80004]: shifted to the top of the word, offset so the window starts at 0
-      risky |= (__float_as_uint(q[j]) << 12) + 0x80004000u <= 0x8000u;
-      risky |= fabsf(x[j]) < subnormal_below;               // subnormal range of e4m3 (also catches exact zeros)
+      q[j] = __builtin_fmaf(-__builtin_fmaf(q[j], scale, -x[j]), rinv, q[j]);
+      q[j] = __builtin_fmaf(-__builtin_fmaf(q[j], scale, -x[j]), rinv, q[j]);
     }
-    risky = risky && live;
-    if (__builtin_amdgcn_ballot_w64(risky) != 0) {
-      // second look: a quotient near a boundary that is exact (zero residual x - q0 * scale; ties of short
-      // mantissas are common with bf16 inputs) is the correctly rounded quotient already
-      bool divide = false;
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(divide), 0)) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool near = (__float_as_uint(q[j]) << 12) + 0x80004000u <= 0x8000u;
-        divide |= near && __builtin_fmaf(-q[j], scale, x[j]) != 0.f;
-        divide |= fabsf(x[j]) < subnormal_below;
-      }
-      divide = divide && live;
-      if (__builtin_amdgcn_ballot_w64(divide) != 0) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = x[j] / scale;
-      }
+      for (int j = 0; j < 8; ++j) q[j] = x[j] / scale;
     }
     u32x2 out;
     out[0] = uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false), true));

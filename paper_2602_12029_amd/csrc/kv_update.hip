@@ -126,7 +126,7 @@ __global__ __launch_bounds__(256) void ingest_e4m3_kernel(KvWriteParams p, const
       x[2 * j] = bf16_bits_to_f32(raw[i][j] & 0xffffu);
       x[2 * j + 1] = bf16_bits_to_f32(raw[i][j] >> 16);
     }
-    const u32x2 out = encode(x, c < total);                   // lanes past the tile hold zeros: no say
+    const u32x2 out = encode(x);
     if (c < total) stream_store(reinterpret_cast<u32x2*>(dst + int64_t(token_of(c)) * p.s_tok + column_of(c)), out);
   }
 }

@@ -153,6 +153,7 @@ struct ps_layout {
     std::vector<int32_t> choices, score_items;
     int64_t off_choices = 0, off_score_items = 0;   // in the blob
     int64_t score_words = 0;
+    double reread = 0;               // share of the batch's tokens that another request is likely to read too
     int32_t most_candidates = 0;
   };
   std::unique_ptr<selection> sel;

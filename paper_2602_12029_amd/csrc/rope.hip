@@ -124,7 +124,9 @@ __device__ __forceinline__ void norm8(float (&x)[8], const float (&w)[8], float 
   for (int j = 0; j < 8; ++j) x[j] = (x[j] * inv) * w[j];
 }
 
-// The rotation of a row's elements 8 c8 .. 8 c8 + 7, its pairs' cosines and sines in LDS.  All lanes of the wave come here.
+// The rotation of a row's elements 8 c8 .. 8 c8 + 7 (L lanes to a row), its pairs' cosines and sines in LDS, on a 16-byte boundary
+// where pairs are halves.  All lanes of the wave come here.
+template <int L>
 __device__ __forceinline__ void rotate8(float (&x)[8], int c8, const float* cosines, const float* sines, int rot, bool neighbours) {
   const int c = 8 * c8, half = rot >> 1;
   if (neighbours) {
@@ -139,16 +141,26 @@ __device__ __forceinline__ void rotate8(float (&x)[8], int c8, const float* cosi
   }
   // (half a multiple of 8: the partners of a lane's elements are all in one other lane of the row)
   const bool second = c >= half;
-  const int lane = threadIdx.x & 63, from = c >= rot ? lane : second ? lane - (half >> 3) : lane + (half >> 3);
-  const int i = c >= rot ? 0 : second ? c - half : c;
   float other[8];
+  if (L == 16 && rot == 8 * L) {   // whole rows of 16 lanes: a rotation by 8 of them
 #pragma unroll
-  for (int j = 0; j < 8; ++j) other[j] = __int_as_float(__builtin_amdgcn_ds_bpermute(from << 2, __float_as_int(x[j])));
+    for (int j = 0; j < 8; ++j) other[j] = __uint_as_float(dpp_u32<kRor8>(0, __float_as_uint(x[j])));
+  } else {
+    const int lane = threadIdx.x & 63, from = c >= rot ? lane : second ? lane - (half >> 3) : lane + (half >> 3);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) other[j] = __int_as_float(__builtin_amdgcn_ds_bpermute(from << 2, __float_as_int(x[j])));
+  }
   if (c < rot) {
+    const int i = second ? c - half : c;
+    const uint32_t sign = second ? 0u : 0x80000000u;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float co = cosines[i + j], si = sines[i + j];
-      x[j] = __builtin_fmaf(x[j], co, (second ? other[j] : -other[j]) * si);
+    for (int j = 0; j < 8; j += 4) {
+      const f32x4 co = *reinterpret_cast<const f32x4*>(cosines + i + j), si = *reinterpret_cast<const f32x4*>(sines + i + j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float turned = __uint_as_float(__float_as_uint(si[e]) ^ sign);
+        x[j + e] = __builtin_fmaf(x[j + e], co[e], other[j + e] * turned);
+      }
     }
   }
 }
@@ -176,7 +188,7 @@ template <int D, typename T, int UNITS>
 __global__ __launch_bounds__(256) void rope_rows_kernel(RopeArgs a, const T* __restrict__ src, int64_t s_row, int64_t s_head,
                                                         T* __restrict__ out, int64_t row0, int64_t num_waves, int heads, int groups) {
   constexpr int L = D / 8, kHeads = 64 / L;   // lanes of a head row, head rows a wave holds at a time
-  __shared__ float sm[4][2][D / 2];
+  __shared__ __attribute__((aligned(16))) float sm[4][2][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), c8 = lane & (L - 1);
   const int64_t id = int64_t(blockIdx.x) * 4 + wave;
   if (id >= num_waves) return;
@@ -193,7 +205,7 @@ __global__ __launch_bounds__(256) void rope_rows_kernel(RopeArgs a, const T* __r
     float x[8];
     widen8(raw[u], x);
     if (a.q_weight) norm8<L>(x, w, a.eps);
-    rotate8(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
+    rotate8<L>(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
     const int h = h0 + u * kHeads;
     if (h < heads) store8(out + (t * heads + h) * D + 8 * c8, narrow8<T>(x));
   }
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
                                                           int64_t s_row_kv, int64_t s_head_kv, QT* __restrict__ q_out, int num_q_heads) {
   typedef std::conditional_t<KVT == PS_F32, float, uint16_t> T;
   constexpr int L = D / 8, kHeads = 64 / L;
-  __shared__ float sm[4][2][D / 2];
+  __shared__ __attribute__((aligned(16))) float sm[4][2][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), c8 = lane & (L - 1);
   const int r = blockIdx.x;
   const int nq = q ? (num_q_heads + kHeads - 1) / kHeads : 0;
@@ -221,7 +233,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
     wave_angles<D>(a, a.positions[r], sm[wave][0], sm[wave][1]);
     widen8(raw, x);
     if (a.q_weight) norm8<L>(x, w, a.eps);
-    rotate8(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
+    rotate8<L>(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
     if (h < num_q_heads) store8(q_out + (int64_t(r) * num_q_heads + h) * D + 8 * c8, narrow8<QT>(x));
     return;
   }
@@ -242,7 +254,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
       load_weight<T>(a.k_weight, c8, w);
       wave_angles<D>(a, a.positions[r], sm[wave][0], sm[wave][1]);
       if (a.k_weight) norm8<L>(x, w, a.eps);
-      rotate8(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
+      rotate8<L>(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
     }
     append_e4m3x8_values(p, tile, x, old, __builtin_ctz(L));
   } else {
@@ -258,7 +270,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
       wave_angles<D>(a, a.positions[r], sm[wave][0], sm[wave][1]);
       widen8(raw, x);
       if (a.k_weight) norm8<L>(x, w, a.eps);
-      rotate8(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
+      rotate8<L>(x, c8, sm[wave][0], sm[wave][1], a.rot, a.neighbours);
       raw = narrow8<T>(x);
     }
     T* dst = static_cast<T*>(p.kv) + int64_t(dest / p.block_size) * p.s_block + int64_t(h) * p.s_head + int64_t(which) * p.s_kv +
@@ -272,11 +284,11 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
 // through its (head, K|V) tiles, WPT waves to a tile, CH eight-element pieces a lane.  HBM-bound.  The angles of the pass's
 // tokens lie in LDS for all heads.
 template <int D, int KVT, int CH, int WPT>
-__global__ __launch_bounds__(256) void ingest_rope_kernel(RopeArgs a, KvWriteParams p, const void* __restrict__ src_k, const void* __restrict__ src_v,
+__global__ __launch_bounds__(256, CH == 4 && KVT == PS_FP8_E4M3 ? 4 : 2) void ingest_rope_kernel(RopeArgs a, KvWriteParams p, const void* __restrict__ src_k, const void* __restrict__ src_v,
                                                           int64_t s_tok, int64_t s_head, int entry0, int passes, int tiles_per_team) {
   typedef std::conditional_t<KVT == PS_F32, float, uint16_t> T;
   constexpr int L = D / 8, kTeams = 4 / WPT, kPass = CH * WPT * 64 / L;   // tokens the teams hold of a tile
-  extern __shared__ float angles[];                                       // [kPass][2][rot / 2]: cosines, sines
+  extern __shared__ __attribute__((aligned(16))) float angles[];                                      // [kPass][2][rot / 2]: cosines, sines
   __shared__ float sm_max[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), c8 = lane & (L - 1);
   const int e = p.ent_order[entry0 + int(blockIdx.x) / passes];
@@ -298,9 +310,10 @@ __global__ __launch_bounds__(256) void ingest_rope_kernel(RopeArgs a, KvWritePar
   Raw8<T> raw[CH];
   fetch(min(tile, num_tiles - 1), raw);
   if (int(blockIdx.y) * tiles_per_team * kTeams < p.num_kv_heads) {   // (V tiles alone need no angles)
-    for (int i = threadIdx.x; i < count * half; i += 256) {
-      const int t = i / half, pair = i - t * half;
-      turn_sincos(turn_of(a.positions[tok0 + t], a.turns[pair]), angles[(2 * t + 1) * half + pair], angles[2 * t * half + pair]);
+    // a pair a lane, a token a wave
+    for (int pair = lane; pair < half; pair += 64) {
+      const uint64_t rate = a.turns[pair];
+      for (int t = wave; t < count; t += 4) turn_sincos(turn_of(a.positions[tok0 + t], rate), angles[(2 * t + 1) * half + pair], angles[2 * t * half + pair]);
     }
     __syncthreads();
   }
@@ -309,21 +322,21 @@ __global__ __launch_bounds__(256) void ingest_rope_kernel(RopeArgs a, KvWritePar
   // (a team without a tile of its own still meets the others of a WPT = 4 tile: there all waves are one team)
   for (; tile < tile_end; tile += kTeams) {
     const int which = tile >= p.num_kv_heads, h = which ? tile - p.num_kv_heads : tile;
-    float x[CH][8];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) widen8(raw[i], x[i]);
-    if (tile + kTeams < tile_end) fetch(tile + kTeams, raw);
-    if (which == 0) {
-#pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        const int t = min(lane_tok + i * kStep, count - 1);
-        if (a.k_weight) norm8<L>(x[i], w, a.eps);
-        rotate8(x[i], c8, angles + 2 * t * half, angles + (2 * t + 1) * half, a.rot, a.neighbours);
-      }
-    }
     const int64_t at = int64_t(id) * p.s_block + int64_t(h) * p.s_head + int64_t(which) * p.s_kv + int64_t(first) * p.s_tok + 8 * c8;
+    auto turned = [&](float (&x)[8], int i) {
+      const int t = min(lane_tok + i * kStep, count - 1);
+      if (a.k_weight) norm8<L>(x, w, a.eps);
+      rotate8<L>(x, c8, angles + 2 * t * half, angles + (2 * t + 1) * half, a.rot, a.neighbours);
+    };
     if constexpr (KVT == PS_FP8_E4M3) {
-      float amax = 0.f;
+      float x[CH][8], amax = 0.f;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) widen8(raw[i], x[i]);
+      if (tile + kTeams < tile_end) fetch(tile + kTeams, raw);
+      if (which == 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) turned(x[i], i);
+      }
 #pragma unroll
       for (int i = 0; i < CH; ++i)
         if (lane_tok + i * kStep < count) {
@@ -344,10 +357,18 @@ __global__ __launch_bounds__(256) void ingest_rope_kernel(RopeArgs a, KvWritePar
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int t = lane_tok + i * kStep;
-        const u32x2 codes = encode(x[i], t < count);
+        const u32x2 codes = encode(x[i]);
         if (t < count) stream_store(reinterpret_cast<u32x2*>(static_cast<uint8_t*>(p.kv) + at + int64_t(t) * p.s_tok), codes);
       }
     } else {
+      float x[CH][8];
+#pragma unroll
+      for (int i = 0; i < CH; ++i) widen8(raw[i], x[i]);
+      if (tile + kTeams < tile_end) fetch(tile + kTeams, raw);
+      if (which == 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) turned(x[i], i);
+      }
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int t = lane_tok + i * kStep;

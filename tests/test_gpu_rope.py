@@ -368,3 +368,37 @@ def test_a_captured_step_replays(gpu):
         assert torch.equal(eager.batch.scales.view(torch.int32), replayed.batch.scales.view(torch.int32))
     eager.close()
     replayed.close()
+
+
+@pytest.mark.parametrize("magnitude", [2.0 ** -130, 2.0 ** -120, 2.0 ** -95, 2.0 ** -82, 1.0, 2.0 ** 90, 2.0 ** 126])
+def test_tiles_of_extreme_magnitude(gpu, magnitude):
+    """e4m3 tiles whose scale is subnormal, tiny or huge, zeros of both signs among them: the bits of the oracle's quantiser, by the plain
+    ingest and by the fused one."""
+    from oracle import kv_update as ku
+    from paper_2602_12029_amd.runtime import Rope
+    w = wl.make_workload("extreme", wl.Geometry(4, 2, 128, 16, "bf16", "fp8_e4m3"), 1, [70], [[0]], [0], seed=3)
+    case = gpu(w)
+    rng = np.random.default_rng(4)
+    src = []
+    for _ in range(2):
+        x = rng.uniform(-1, 1, (70, 2, 128)) * np.exp2(-rng.integers(0, 16, (70, 2, 128)).astype(float))
+        x[rng.random(x.shape) < 0.05] = 0.0
+        x[rng.random(x.shape) < 0.05] = -0.0
+        src.append(wl.bf16_bits_from_f32((x * magnitude).astype(np.float32)))
+    from paper_2602_12029_amd.runtime import to_device
+    k, v = (to_device(s, "bf16") for s in src)
+    _poison(case)
+    case.data.kv[...] = 0xff
+    case.data.scales[...] = np.nan
+    ku.ingest_segment(case.data.kv, case.data.scales, "fp8_e4m3", case.olay.prefix_blk, *src)
+    for fused in (False, True):
+        _poison(case)
+        if fused:
+            case.batch.kv_ingest_rope(0, Rope([]), k, v, torch.zeros(70, dtype=torch.int32, device="cuda"))
+        else:
+            case.batch.kv_ingest(0, k, v)
+        torch.cuda.synchronize()
+        ids = case.olay.prefix_blk
+        assert np.array_equal(case.batch.scales.cpu().numpy()[ids].view(np.int32), case.data.scales[ids].view(np.int32)), fused
+        assert np.array_equal(case.batch.kv.cpu().numpy(), case.data.kv), fused
+    case.close()
