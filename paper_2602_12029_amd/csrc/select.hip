@@ -86,8 +86,8 @@ __device__ __forceinline__ float rows_max(const float* v) {
 // item, block ids, summaries; the query rows go the same way beside it, all under way before the codes are worked out.
 // 64 / 128 / 256 blocks a workgroup, eight heads: 32 thousand blocks under three requests 24.1 / 20.1 / 20.7 us, 105 thousand under four
 // 73.5 / 60.3 / 60.1, 8.7 thousand 10.6 / 9.7 / 10.6, 31 thousand under one 17.1 / 15.9 / 15.9; in rounds, four workgroups a compute unit,
-// 22.6 / 70.4 / 10.9 / 15.4.  What bounds it is the vector unit (537 instructions a wave with 32 rows, the codes of the rows and
-// the maxima most of them, 24 of the 60 us) and the memory behind the chain.
+// 22.6 / 70.4 / 10.9 / 15.4.  What bounds it is memory that is read 256 bytes a block at a time, blocks anywhere: 105 thousand blocks under
+// one request 50 us, 4.2 TB/s, whether the loads cover whole 128-byte lines or halves of them, whatever the order of the heads.
 template <int D, typename QT, int ROWS>
 __global__ __launch_bounds__(256) void score_kernel(SelectParams p) {
   constexpr int kRowBytes = 2 * D, kLdsRow = kRowBytes + 16, kSteps = kRowBytes / 64, kPer = D / 16, NT = kPsScoreBlocks / 64;
@@ -259,6 +259,7 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(SelectParams p) {
   auto block_at = [&](int j) { return p.blk[j < c.num_root ? c.root_entry + j : c.prefix_entry + j - c.num_root]; };
   uint32_t key[kHeld];
   int32_t id[kHeld], slot[kHeld];
+  uint32_t bin_at[kHeld];   // of the keys in question; the others: none
   // every position with its key, in any order
   auto each = [&](auto&& f) {
     if constexpr (PER > 0) {
@@ -326,9 +327,13 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(SelectParams p) {
     const float per_unit = linear ? float(kBins - 1) / width : 0.f;
     const int bits = range ? 32 - __builtin_clz(range) : 0, shift = bits > 8 ? bits - 8 : 0;
     auto bin_of = [&](uint32_t k) { return linear ? min(uint32_t((value_of(k) - bottom) * per_unit), uint32_t(kBins - 1)) : (k - low) >> shift; };
-    each([&](int, int, uint32_t k) {
-      if (k >= low && k <= high) atomicAdd(&sm_bins[bin_of(k)], 1u);
+    each([&](int u, int, uint32_t k) {
+      const uint32_t bin = k >= low && k <= high ? bin_of(k) : kTaken;
+      bin_at[u] = bin;
+      if (bin < uint32_t(kBins)) atomicAdd(&sm_bins[bin], 1u);
     });
+    // (again, where they are not held)
+    auto in = [&](int u, uint32_t k, uint32_t bin) { return PER > 0 ? bin_at[u] == bin : k >= low && k <= high && bin_of(k) == bin; };
     __syncthreads();
     // from the top: lane i of every wave holds bins 255 - 4 i .. 252 - 4 i
     uint32_t mine[4], sum = 0;
@@ -354,7 +359,7 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(SelectParams p) {
     need -= int(over);
     if (in_bin <= uint32_t(kFew)) {
       each([&](int u, int j, uint32_t k) {
-        if (k >= low && k <= high && bin_of(k) == bin) {
+        if (in(u, k, bin)) {
           const uint32_t i = atomicAdd(&sm_n, 1u);
           sm_few[i] = uint64_t(k) << 32 | uint32_t(~j);
           if constexpr (PER > 0) slot[u] = int(i);
@@ -382,8 +387,8 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(SelectParams p) {
       break;
     }
     uint32_t bin_low = 0xffffffffu, bin_high = 0;
-    each([&](int, int, uint32_t k) {
-      if (k >= low && k <= high && bin_of(k) == bin) {
+    each([&](int u, int, uint32_t k) {
+      if (in(u, k, bin)) {
         bin_low = min(bin_low, k);
         bin_high = max(bin_high, k);
       }
