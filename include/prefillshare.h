@@ -374,7 +374,7 @@ typedef struct ps_rope {
 /* ps_rope_turns (host): out[i] = radians[i] / (2 pi) modulo 1, times 2^64; radians: angle per position, finite, >= 0. */
 int32_t ps_rope_turns(int32_t count, const double* radians, uint64_t* out);
 /* ps_rope_rows (device, asynchronous): the queries of any number of tokens (those of a partial prefill): src row t, head h at
- * t * src_stride_row + h * src_stride_head (strides in elements, multiples of 16 bytes, pointers 16-byte aligned), q_dtype,
+ * t * src_stride_row + h * src_stride_head (strides in elements, at least head_dim, multiples of 16 bytes, pointers 16-byte aligned), q_dtype,
  * num_q_heads heads; out [num_rows][Hq][d] contiguous, which may be src itself where that is contiguous; positions: device
  * int32[num_rows].  Norm with q_weight. */
 int32_t ps_rope_rows(const ps_geometry* geometry, const ps_rope* rope, int64_t num_rows, const void* src, int64_t src_stride_row,
@@ -439,7 +439,8 @@ typedef struct ps_select_options {
  * with PS_ERR_INVALID_ARG.  PS_ERR_UNSUPPORTED: more than 64 query heads per KV head, contexts of more than 65536 blocks, another
  * head_dim than 64, 128, 256.
  * ps_layout_select_follow (host): brings a selection in line with its base after ps_layout_append, ps_layout_set_visible or
- * ps_layout_replan there; upload it again afterwards.  An append that leaves the plan's structure alone is patched in, as there. */
+ * ps_layout_replan there; upload it again afterwards, and choose anew: its lists start again.  An append that leaves the plan's structure
+ * alone is patched in, as there.  After a follow that fails the selection refuses its passes, its merge and a replan until one succeeds. */
 int32_t ps_layout_select(const ps_layout* base, const ps_select_options* options, ps_layout** out);
 int32_t ps_layout_select_follow(const ps_layout* base, ps_layout* selection);
 /* Where the lists lie in the selection's uploaded tables (host views, valid until the next follow/release): request r's list for
@@ -452,7 +453,7 @@ int64_t ps_select_workspace_bytes(const ps_layout* selection);
  * q / s_q with s_q from max |q| as for the summaries (what is not a number counts as 0).  The score of a block for a request and
  * KV head is the largest over the group's query heads of (float(sum over c of max(q_c, 0) hi_c + min(q_c, 0) lo_c) * s_block) * s_q:
  * a whole number under 2^24 and two float32 products, so a choice is the same bits wherever it is made.  The highest scores are
- * taken, the lower position first where they are equal.  base_tables, selection_tables: current uploads of both; base must be what
+ * taken, the lower position first where they are equal; one that is not a number (of a block whose scale is none) counts as the lowest.  base_tables, selection_tables: current uploads of both; base must be what
  * the selection last followed (PS_ERR_INVALID_ARG). */
 int32_t ps_select_blocks(const ps_layout* base, const void* base_tables, const ps_layout* selection, void* selection_tables,
                          const void* q, const int8_t* summaries, const float* summary_scales, void* workspace, void* stream);

@@ -11,7 +11,7 @@ implementation can match bit for bit:
   * query codes likewise per row (what is not a number counts as 0).
   * score(r, h, j) = max over the heads g of KV head h of (float32(sum_c max(q_gc, 0) hi_jc + min(q_gc, 0) lo_jc) * s_j) * s_g.
   * Of a request's context (root blocks, then the visible blocks of its prefix) `blocks` are taken: the first keep_first, the last
-    keep_last, a root's partly filled last block, and the highest scores, lower positions first where they are equal; all of a context
+    keep_last, a root's partly filled last block, and the highest scores, lower positions first where they are equal (no number: the lowest); all of a context
     of no more than that.
 """
 from __future__ import annotations
@@ -94,6 +94,7 @@ def choose(score: np.ndarray, n: int, partial: int, blocks: int, keep_first: int
     if len(others) <= most:
         return others
     always = [j for j in others if j < keep_first or j >= n - keep_last]
+    score = np.where(np.isnan(score), -np.inf, score)
     rest = sorted((j for j in others if keep_first <= j < n - keep_last), key=lambda j: (-float(score[j]), j))
     return sorted(always + rest[:most - len(always)])
 

@@ -294,7 +294,7 @@ int32_t ps_suffix_attention(const ps_layout* lay, const void* dev_tables, const 
 
 int32_t ps_merge_states(const ps_layout* lay, const void* dev_tables, const void* workspace, void* out,
                         float* out_lse, void* stream) {
-  if (!lay || !dev_tables || !workspace) return PS_ERR_INVALID_ARG;
+  if (!lay || !dev_tables || !workspace || (lay->sel && lay->parked)) return PS_ERR_INVALID_ARG;
   if (lay->num_requests && !out) return PS_ERR_INVALID_ARG;
   const psdev::AttnParams p = make_params(lay, dev_tables, nullptr, nullptr, nullptr, const_cast<void*>(workspace));
   if (int32_t rc = psdev::launch_merge(p.slot_base, nullptr, p.ws_o, p.ws_lse, out, out_lse, lay->num_requests,

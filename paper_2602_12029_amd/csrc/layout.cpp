@@ -1572,7 +1572,7 @@ int32_t ps_layout_request_list(const ps_layout* lay, int32_t* count, const int32
 }
 
 int32_t ps_layout_replan(ps_layout* lay, const ps_plan_options* options) {
-  if (!lay) return PS_ERR_INVALID_ARG;
+  if (!lay || (lay->sel && lay->parked)) return PS_ERR_INVALID_ARG;   // (a selection whose follow failed has half of a batch)
   return ps_plan_build(lay, options);
 }
 
@@ -1693,7 +1693,9 @@ int32_t derive_selection(const ps_layout* base, ps_layout* lay) {
       }
     }
     lay->prefix_blk_indptr[size_t(r) + 1] = int32_t(lay->prefix_blk.size());
-    lay->prefix_len[size_t(r)] = c.count * B - (seen % B ? B - seen % B : 0);
+    const int64_t tokens = int64_t(c.count) * B - (seen % B ? B - seen % B : 0);
+    if (tokens > INT32_MAX) return PS_ERR_UNSUPPORTED;
+    lay->prefix_len[size_t(r)] = int32_t(tokens);
     if (c.skip >= 0) {
       lay->prompt_root[size_t(r)] = lay->num_roots++;
       lay->root_len.push_back(root_len % B);
@@ -1789,19 +1791,26 @@ int32_t ps_layout_select(const ps_layout* base, const ps_select_options* options
 
 int32_t ps_layout_select_follow(const ps_layout* base, ps_layout* lay) {
   if (!base || !lay || !lay->sel || base->parked || lay->sel->base_id != base->id) return PS_ERR_INVALID_ARG;
-  lay->parked = true;   // (where it fails half-way nothing may be launched from it; the next follow mends it)
+  lay->parked = true;   // (where it fails half-way nothing may be launched from it; the next follow plans it anew)
+  int32_t rc = PS_ERR_OOM;
   try {
     const std::vector<int32_t> prefix_len = lay->prefix_len, root_len = lay->root_len, suffix_len = lay->suffix_len;
     const std::vector<int32_t> prompt_root = lay->prompt_root;
     const int64_t old_stride = lay->head_stride;
     lay->sel->base_version = 0;
-    if (int32_t st = derive_selection(base, lay)) return st;
-    bool grown = prefix_len == lay->prefix_len && root_len == lay->root_len && prompt_root == lay->prompt_root;
-    for (size_t r = 0; r < suffix_len.size() && grown; ++r) grown = unsigned(lay->suffix_len[r] - suffix_len[r]) <= 1;
-    auto grew = [&](int32_t r) { return lay->suffix_len[size_t(r)] != suffix_len[size_t(r)]; };
-    if (int32_t st = grown ? plan_growth(lay, grew, old_stride) : ps_plan_build(lay, &lay->opt)) return st;
+    rc = derive_selection(base, lay);
+    if (rc == PS_OK) {
+      bool grown = prefix_len == lay->prefix_len && root_len == lay->root_len && prompt_root == lay->prompt_root;
+      for (size_t r = 0; r < suffix_len.size() && grown; ++r) grown = unsigned(lay->suffix_len[r] - suffix_len[r]) <= 1;
+      auto grew = [&](int32_t r) { return lay->suffix_len[size_t(r)] != suffix_len[size_t(r)]; };
+      rc = grown ? plan_growth(lay, grew, old_stride) : ps_plan_build(lay, &lay->opt);
+    }
   } catch (const std::bad_alloc&) {
-    return PS_ERR_OOM;
+    rc = PS_ERR_OOM;
+  }
+  if (rc != PS_OK) {
+    lay->suffix_chunks.clear();
+    return rc;
   }
   lay->sel->base_version = base->version;
   lay->parked = false;

@@ -284,7 +284,7 @@ __global__ __launch_bounds__(THREADS) void choose_kernel(SelectParams p) {
 
   uint32_t low = 0xffffffffu, high = 0;
   auto key_of = [&](float v, int j) {
-    const uint32_t order = order_of(v + 0.f);   // (-0 counts as 0)
+    const uint32_t order = order_of(v == v ? v + 0.f : -__builtin_inff());   // (-0 counts as 0, and no number, from scales that are none, as the lowest)
     const bool open = j >= c.first && j < c.last && j != c.skip;
     if (open) {
       low = min(low, order);
@@ -501,7 +501,7 @@ int32_t launch_select_blocks(const ps_layout* base, const void* dev_tables, cons
   p.num_kv_heads = g.num_kv_heads;
   p.group = g.num_q_heads / g.num_kv_heads;
   const int64_t n_items = int64_t(s.score_items.size() * 4 / sizeof(ps_score_item)), n_choices = int64_t(s.choices.size() * 4 / sizeof(ps_choice));
-  if (n_items * g.num_kv_heads > kMaxWorkgroups || n_choices * g.num_kv_heads > kMaxWorkgroups) return PS_ERR_UNSUPPORTED;
+  if (n_items * g.num_kv_heads > kMaxWorkgroups || n_choices * g.num_kv_heads > kMaxWorkgroups / 4) return PS_ERR_UNSUPPORTED;   // (up to 1024 threads)
   const dim3 grid(unsigned(n_items * g.num_kv_heads));
 #define PS_SCORE(D, T, ROWS) hipLaunchKernelGGL((score_kernel<D, T, ROWS>), grid, dim3(256), 0, st, p)
 #define PS_SCORE_C(D, T)                                                                                                          \

@@ -43,28 +43,43 @@ class Rope:
 
     def __init__(self, radians, pairing="halves", q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
                  eps: float = 1e-6, device="cuda:0"):
-        for w in (q_weight, k_weight):
-            if w is not None and not w.is_contiguous():
-                raise ValueError("norm weights are contiguous tensors")
         turns = B.ps_rope_turns(radians)
-        self.turns = torch.from_numpy(turns.view(np.int64)).to(device) if turns.size else None
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.device = self.turns.device
+        for w in (q_weight, k_weight):
+            if w is not None and (not w.is_contiguous() or w.device != self.device):
+                raise ValueError(f"norm weights are contiguous tensors on {self.device}")
         self.q_weight, self.k_weight = q_weight, k_weight
         self.struct = B.ps_rope(self.turns.data_ptr() if turns.size else 0, q_weight.data_ptr() if q_weight is not None else 0,
                                 k_weight.data_ptr() if k_weight is not None else 0, eps, 2 * turns.size, B.PAIRING.get(pairing, pairing))
 
+    def check(self, device: torch.device, dim: int, q_dtype: torch.dtype | None, k_dtype: torch.dtype | None):
+        """Refuses rows of another device, or weights that are not one row of their type."""
+        if device != self.device:
+            raise ValueError(f"the rotation's parameters are on {self.device}, the rows on {device}")
+        for name, w, dtype in (("q_weight", self.q_weight, q_dtype), ("k_weight", self.k_weight, k_dtype)):
+            if w is not None and dtype is not None and (w.dtype is not dtype or w.shape != (dim,)):
+                raise ValueError(f"{name}: [{dim}] of {dtype} is wanted")
 
-def _row_strides(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, dim: int):
+
+def _row_strides(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, dim: int, device: torch.device):
     """(row, head) strides of rows [rows, heads, dim] with contiguous elements; anything else is refused."""
     strides = t.stride()
-    if t.dtype is not dtype or t.shape != (rows, heads, dim) or strides[2] != 1:
-        raise ValueError(f"{name}: rows [{rows}, {heads}, {dim}] of {dtype} with contiguous elements are wanted")
+    if t.dtype is not dtype or t.shape != (rows, heads, dim) or strides[2] != 1 or t.device != device:
+        raise ValueError(f"{name}: rows [{rows}, {heads}, {dim}] of {dtype} with contiguous elements on {device} are wanted")
     # (of an axis of one the stride is not used, and torch's may be anything)
     return strides[0] if rows > 1 else max(strides[0], dim), strides[1] if heads > 1 else max(strides[1], dim)
 
 
-def _check_positions(t: torch.Tensor, rows: int):
-    if t.dtype is not torch.int32 or t.shape != (rows,) or (rows > 1 and t.stride(0) != 1):
-        raise ValueError(f"positions: a contiguous int32 tensor of {rows} is wanted")
+def _check_positions(t: torch.Tensor, rows: int, device: torch.device):
+    if t.dtype is not torch.int32 or t.shape != (rows,) or (rows > 1 and t.stride(0) != 1) or t.device != device:
+        raise ValueError(f"positions: a contiguous int32 tensor of {rows} on {device} is wanted")
+
+
+def _current(device: torch.device):
+    """Launches go to the current device's current stream: a batch of another device is not served from here."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, which is not the current device")
 
 
 _TORCH_DTYPE = {B.PS_F32: torch.float32, B.PS_BF16: torch.bfloat16}
@@ -73,12 +88,14 @@ _TORCH_DTYPE = {B.PS_F32: torch.float32, B.PS_BF16: torch.bfloat16}
 def rope_rows(geometry: B.ps_geometry, rope: Rope, src: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """Queries of any number of tokens [T, Hq, d] normed and rotated; returns them contiguous (in `out` where given)."""
     dtype, n = _TORCH_DTYPE[geometry.q_dtype], src.shape[0]
-    row, head = _row_strides("src", src, dtype, n, geometry.num_q_heads, geometry.head_dim)
-    _check_positions(positions, n)
+    row, head = _row_strides("src", src, dtype, n, geometry.num_q_heads, geometry.head_dim, src.device)
+    _check_positions(positions, n, src.device)
     if out is None:
         out = torch.empty(src.shape, dtype=dtype, device=src.device)
-    elif out.shape != src.shape or out.dtype is not dtype or not out.is_contiguous():
+    elif out.shape != src.shape or out.dtype is not dtype or not out.is_contiguous() or out.device != src.device:
         raise ValueError("out: a contiguous tensor like src is wanted")
+    rope.check(src.device, geometry.head_dim, dtype, None)
+    _current(src.device)
     B.ps_rope_rows(geometry, rope.struct, n, src.data_ptr(), row, head, positions.data_ptr(), out.data_ptr(), _stream())
     return out
 
@@ -168,6 +185,8 @@ class DecodeBatch:
         """The tokens reserved by the last append, from raw projections [R, heads, d]: queries normed and rotated into self.q (q None:
         left alone), keys normed and rotated and values into the cache."""
         rows = self._token_rows(q, k, v, positions)
+        rope.check(self.device, self.geometry.head_dim, self.q.dtype if q is not None else None, k.dtype)
+        _current(self.device)
         B.ps_kv_append_rope(self.layout, self.tables.data_ptr(), rope.struct, rows, self.q.data_ptr() if q is not None else 0,
                             self.kv.data_ptr(), self._sc(), self._stream())
 
@@ -175,13 +194,13 @@ class DecodeBatch:
         g, n = self.geometry, self.num_requests
         heads, d = g.num_kv_heads, g.head_dim
         dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
-        strides = _row_strides("k", k, dtype, n, heads, d)
-        if _row_strides("v", v, dtype, n, heads, d) != strides:
+        strides = _row_strides("k", k, dtype, n, heads, d, self.device)
+        if _row_strides("v", v, dtype, n, heads, d, self.device) != strides:
             raise ValueError("k and v have the same strides")
-        _check_positions(positions, n)
+        _check_positions(positions, n, self.device)
         if q is None:
             return B.ps_token_rows(0, k.data_ptr(), v.data_ptr(), 0, 0, *strides, positions.data_ptr())
-        q_strides = _row_strides("q", q, _TORCH_DTYPE[g.q_dtype], n, g.num_q_heads, d)
+        q_strides = _row_strides("q", q, _TORCH_DTYPE[g.q_dtype], n, g.num_q_heads, d, self.device)
         if not self.q.is_contiguous():
             raise ValueError("the batch's queries are a contiguous tensor")
         return B.ps_token_rows(q.data_ptr(), k.data_ptr(), v.data_ptr(), *q_strides, *strides, positions.data_ptr())
@@ -191,10 +210,12 @@ class DecodeBatch:
         g, n = self.geometry, self._segment_tokens(which)
         heads, d = g.num_kv_heads, g.head_dim
         dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
-        strides = _row_strides("src_k", src_k, dtype, n, heads, d)
-        if _row_strides("src_v", src_v, dtype, n, heads, d) != strides:
+        strides = _row_strides("src_k", src_k, dtype, n, heads, d, self.device)
+        if _row_strides("src_v", src_v, dtype, n, heads, d, self.device) != strides:
             raise ValueError("src_k and src_v have the same strides")
-        _check_positions(positions, n)
+        _check_positions(positions, n, self.device)
+        rope.check(self.device, d, None, dtype)
+        _current(self.device)
         B.ps_kv_ingest_rope(self.layout, self.tables.data_ptr(), which, rope.struct, src_k.data_ptr(), src_v.data_ptr(), *strides,
                             positions.data_ptr(), self.kv.data_ptr(), self._sc(), self._stream())
 
@@ -204,9 +225,10 @@ class DecodeBatch:
         heads, d = g.num_kv_heads, g.head_dim
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise ValueError("dst_k, dst_v: bf16 or float32 tensors are wanted")
-        strides = _row_strides("dst_k", dst_k, dtype, n, heads, d)
-        if _row_strides("dst_v", dst_v, dtype, n, heads, d) != strides:
+        strides = _row_strides("dst_k", dst_k, dtype, n, heads, d, self.device)
+        if _row_strides("dst_v", dst_v, dtype, n, heads, d, self.device) != strides:
             raise ValueError("dst_k and dst_v have the same strides")
+        _current(self.device)
         B.ps_kv_gather(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(),
                        B.PS_F32 if dtype is torch.float32 else B.PS_BF16, dst_k.data_ptr(), dst_v.data_ptr(), *strides, self._stream())
 
@@ -217,14 +239,16 @@ class DecodeBatch:
     def block_summaries(self, which: int, summaries: torch.Tensor, summary_scales: torch.Tensor):
         """Eight-bit bounds of every block's keys: summaries int8 [num_blocks, Hkv, 2, d], summary_scales float32 [num_blocks, Hkv]."""
         self._check_summaries(summaries, summary_scales)
+        _current(self.device)
         B.ps_block_summaries(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(), summaries.data_ptr(),
                              summary_scales.data_ptr(), self._stream())
 
     def _check_summaries(self, summaries, summary_scales):
         heads, n = self.geometry.num_kv_heads, summaries.shape[0]
         if (summaries.dtype is not torch.int8 or summary_scales.dtype is not torch.float32 or summaries.shape != (n, heads, 2, self.geometry.head_dim) or
-                summary_scales.shape != (n, heads) or not summaries.is_contiguous() or not summary_scales.is_contiguous()):
-            raise ValueError("summaries: contiguous int8 [num_blocks, Hkv, 2, d] and float32 [num_blocks, Hkv] are wanted")
+                summary_scales.shape != (n, heads) or not summaries.is_contiguous() or not summary_scales.is_contiguous() or
+                summaries.device != self.device or summary_scales.device != self.device):
+            raise ValueError(f"summaries: contiguous int8 [num_blocks, Hkv, 2, d] and float32 [num_blocks, Hkv] on {self.device} are wanted")
 
     def select(self, blocks: int, keep_first: int = 1, keep_last: int = 2) -> "SelectedBatch":
         """A step over `blocks` blocks of every request's shared context and its private tokens, chosen by the queries."""
@@ -271,12 +295,21 @@ class DecodeBatch:
 
 class SelectedBatch(DecodeBatch):
     """A selection over a DecodeBatch: its queries and cache, block lists of its own.  select_blocks() chooses, decode_attention() and
-    its parts attend; after append_step, set_visible or replan of the base, follow()."""
+    its parts attend; after append_step, set_visible or replan of the base, follow().  A follow or a replan starts the lists anew:
+    the next step chooses first.  Calls on one selection are ordered by the caller: they share its lists and its scratch memory."""
 
     def __init__(self, base: DecodeBatch, blocks: int, keep_first: int = 1, keep_last: int = 2):
         self.base, self.scratch, self._lists = base, None, None
         layout = B.ps_layout_select(base.layout, blocks, keep_first, keep_last)
         super().__init__(layout, base.geometry, base.num_requests, base.q, base.kv, base.scales)
+
+    @property
+    def q(self) -> torch.Tensor:
+        return self.base.q
+
+    @q.setter
+    def q(self, q: torch.Tensor):
+        self.base.q = q
 
     def _sync_plan(self, wait=True, tokens=None):
         super()._sync_plan(wait, tokens)
@@ -293,8 +326,8 @@ class SelectedBatch(DecodeBatch):
     def select_blocks(self, summaries: torch.Tensor, summary_scales: torch.Tensor):
         """Scores every block of the shared contexts against the base's queries and writes the lists of the highest."""
         self._check_summaries(summaries, summary_scales)
+        _current(self.device)
         base = self.base
-        self.q = base.q
         base._stream()                       # (the base's tables, too, behind their upload)
         B.ps_select_blocks(base.layout, base.tables.data_ptr(), self.layout, self.tables.data_ptr(), base.q.data_ptr(), summaries.data_ptr(),
                            summary_scales.data_ptr(), self.scratch.data_ptr(), self._stream())

@@ -402,3 +402,25 @@ def test_tiles_of_extreme_magnitude(gpu, magnitude):
         assert np.array_equal(case.batch.scales.cpu().numpy()[ids].view(np.int32), case.data.scales[ids].view(np.int32)), fused
         assert np.array_equal(case.batch.kv.cpu().numpy(), case.data.kv), fused
     case.close()
+
+
+@pytest.mark.parametrize("d,block", [(64, 256), (128, 128), (256, 64)])
+def test_the_largest_e4m3_tiles(gpu, d, block):
+    """As many tokens' angles at once as the ingest ever holds, all of their pairs turned."""
+    w = wl.make_workload("large", wl.Geometry(4, 2, d, block, "bf16", "fp8_e4m3"), 1, [2 * block + 9], [[0]], [0], 1.0, seed=3)
+    case = gpu(w)
+    rng = np.random.default_rng(8)
+    n = 2 * block + 9
+    rope, rad, _, kw = _rope(rng, d, "halves", True, d, "bf16")
+    pos = np.arange(n, dtype=np.int32) + 100000
+    k, v = (torch.from_numpy(rng.standard_normal((n, 2, d)).astype(np.float32)).to(torch.bfloat16).cuda() for _ in range(2))
+    _poison(case)
+    case.batch.kv_ingest_rope(0, rope, k, v, torch.from_numpy(pos).cuda())
+    torch.cuda.synchronize()
+    values, scales = _pool(case)
+    ref, mag = _oracle(k, pos, rad, "halves", kw), _magnitude(k, kw)
+    for i, b in enumerate(case.olay.prefix_blk):
+        m = min(block, n - i * block)
+        for h in range(2):
+            _check_tile(values[b, h, 0, :m], scales[b, h, 0], ref[i * block:i * block + m, h], mag[i * block:i * block + m, h], "fp8_e4m3", f"{b} {h}")
+    case.close()

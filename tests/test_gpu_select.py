@@ -185,6 +185,25 @@ def test_equal_scores_and_odd_queries(gpu):
     case.close()
 
 
+def test_scales_that_are_no_numbers(gpu):
+    """Blocks that nobody has summarised: their scales may be anything, and the choice ends all the same, such blocks last."""
+    w = _workload("fp8")
+    case = gpu(w)
+    codes, scales, hcodes, hscales = _summarise(case)
+    rng = np.random.default_rng(2)
+    hcodes, hscales = rng.integers(1, 128, hcodes.shape).astype(np.int8), hscales.copy()   # (no product of 0 with an infinite scale)
+    codes.copy_(torch.from_numpy(hcodes))
+    sel = case.batch.select(9, 1, 2)
+    for share in (0.3, 0.97, 1.0):
+        odd = rng.random(hscales.shape) < share
+        values = np.where(odd, rng.choice(np.array([np.nan, -np.nan, np.inf, -np.inf], np.float32), hscales.shape), hscales).astype(np.float32)
+        scales.copy_(torch.from_numpy(values))
+        sel.select_blocks(codes, scales)
+        with np.errstate(invalid="ignore"):
+            _check_lists(sel, osel.select(_q32(case), case.olay, 16, hcodes, values, 4, 9, 1, 2), f"odd scales {share}")
+    case.close()
+
+
 @pytest.mark.parametrize("blocks_of", [900, 1500, 2049, 3001, 5000, 8192, 8193, 16384, 16385, 20011])
 def test_long_contexts(gpu, blocks_of):
     """Every size of the choice kernel, scores with many equal ones and wide ranges; the lists alone."""

@@ -195,6 +195,37 @@ def test_a_context_of_too_many_blocks():
     B.ps_pool_destroy(pool)
 
 
+def test_a_follow_that_fails():
+    """Nothing is launched from a selection whose follow failed, and the next follow plans it afresh."""
+    geo = B.geometry(4, 1, 64, 16, "bf16", "bf16")
+    n = 65540
+    pool = B.ps_pool_create(n + 64)
+    lay = B.ps_kv_layout(pool, geo, [n * 16, 100], [0, 1], [0, 0], [30, 0])
+    B.ps_layout_set_visible(lay, 2, [900, 100])
+    sel = B.ps_layout_select(lay, 4)
+    for appends in (1, 2, 40):
+        B.ps_layout_set_visible(lay, 2)
+        for _ in range(appends):
+            B.ps_layout_append(pool, lay, 2)
+        _refused(B.PS_ERR_UNSUPPORTED, B.ps_layout_select_follow, lay, sel)
+        _refused(B.PS_ERR_INVALID_ARG, B.ps_layout_replan, sel, B.plan_options())
+        if not HOST_ONLY:                                 # (addresses that nothing may follow)
+            _refused(B.PS_ERR_INVALID_ARG, B.ps_decode_attention, sel, 4096, 4096, 4096, 0, 4096, 4096, 0)
+            _refused(B.PS_ERR_INVALID_ARG, B.ps_merge_states, sel, 4096, 4096, 4096, 0)
+            _refused(B.PS_ERR_INVALID_ARG, B.ps_select_blocks, lay, 4096, sel, 4096, 4096, 4096, 4096, 4096)
+        B.ps_layout_set_visible(lay, 2, [900, 100])
+        B.ps_layout_append(pool, lay, 2)
+        B.ps_layout_select_follow(lay, sel)
+        fresh = B.ps_layout_select(lay, 4)
+        for a, b in ((B.ps_layout_tables(sel, 2, 2), B.ps_layout_tables(fresh, 2, 2)), (B.ps_layout_plan(sel, 2), B.ps_layout_plan(fresh, 2))):
+            assert a.keys() == b.keys() and all(np.array_equal(a[key], b[key]) for key in a)
+        assert np.array_equal(B.ps_select_lists(sel, 2)[0], B.ps_select_lists(fresh, 2)[0])
+        B.ps_layout_release(pool, fresh)
+    for h in (sel, lay):
+        B.ps_layout_release(pool, h)
+    B.ps_pool_destroy(pool)
+
+
 def test_ingest_tokens():
     pool = B.ps_pool_create(64)
     geo = B.geometry(4, 2, 64, 16, "f32", "f32")
@@ -303,12 +334,30 @@ def test_wrappers_check_tensors():
     with pytest.raises(ValueError):
         runtime.Rope(np.ones(32), q_weight=torch.ones(128)[::2], device="cpu")
     b = runtime.DecodeBatch.__new__(runtime.DecodeBatch)
-    b.geometry, b.num_requests, b.q = geo, 5, src
+    b.geometry, b.num_requests, b.q, b.device = geo, 5, src, torch.device("cpu")
     k = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
     for q, kk, v, p in ((src, k, k.float(), pos), (src, k[:4], k[:4], pos), (src.float(), k, k, pos), (src, k, torch.zeros(5, 3, 64, dtype=torch.bfloat16)[:, :2], pos),
                         (src, k, k, pos[::2])):
         with pytest.raises(ValueError):
             b._token_rows(q, kk, v, p)
+    good = b._token_rows(src, k, k, pos)
+    assert (good.q_stride_row, good.q_stride_head, good.kv_stride_row, good.kv_stride_head) == (256, 64, 128, 64)
+    meta = torch.zeros(5, 2, 64, dtype=torch.bfloat16, device="meta")                   # tensors of another device
+    for q, kk, v, p in ((src, meta, k, pos), (src, k, meta, pos), (torch.zeros(5, 4, 64, dtype=torch.bfloat16, device="meta"), k, k, pos),
+                        (src, k, k, torch.zeros(5, dtype=torch.int32, device="meta"))):
+        with pytest.raises(ValueError):
+            b._token_rows(q, kk, v, p)
+    with pytest.raises(ValueError):                                                     # not on a GPU at all
+        b.kv_append_rope(rope, src, k, k, pos)
+    with pytest.raises(ValueError):
+        runtime.rope_rows(geo, rope, src, pos)
+    weights = runtime.Rope(np.ones(32), q_weight=torch.ones(64), k_weight=torch.ones(32, dtype=torch.bfloat16), device="cpu")
+    for q_dtype, k_dtype in ((torch.bfloat16, None), (None, torch.bfloat16)):
+        with pytest.raises(ValueError):
+            weights.check(torch.device("cpu"), 64, q_dtype, k_dtype)
+    weights.check(torch.device("cpu"), 64, torch.float32, None)
+    with pytest.raises(ValueError):
+        runtime.Rope(np.ones(32), q_weight=torch.ones(64, device="meta"), device="cpu")
     for codes, scales in ((torch.zeros(3, 2, 2, 64), torch.zeros(3, 2)), (torch.zeros(3, 2, 2, 64, dtype=torch.int8), torch.zeros(4, 2)),
                           (torch.zeros(3, 2, 64, 2, dtype=torch.int8).transpose(2, 3), torch.zeros(3, 2))):
         with pytest.raises(ValueError):
