@@ -50,6 +50,7 @@ class Rope:
             if w is not None and (not w.is_contiguous() or w.device != self.device):
                 raise ValueError(f"norm weights are contiguous tensors on {self.device}")
         self.q_weight, self.k_weight = q_weight, k_weight
+        self._q, self._k = ((*w.shape, w.dtype) if w is not None else None for w in (q_weight, k_weight))
         self.struct = B.ps_rope(self.turns.data_ptr() if turns.size else 0, q_weight.data_ptr() if q_weight is not None else 0,
                                 k_weight.data_ptr() if k_weight is not None else 0, eps, 2 * turns.size, B.PAIRING.get(pairing, pairing))
 
@@ -57,9 +58,8 @@ class Rope:
         """Refuses rows of another device, or weights that are not one row of their type."""
         if device != self.device:
             raise ValueError(f"the rotation's parameters are on {self.device}, the rows on {device}")
-        for name, w, dtype in (("q_weight", self.q_weight, q_dtype), ("k_weight", self.k_weight, k_dtype)):
-            if w is not None and dtype is not None and (w.dtype is not dtype or w.shape != (dim,)):
-                raise ValueError(f"{name}: [{dim}] of {dtype} is wanted")
+        if (q_dtype is not None and self._q not in (None, (dim, q_dtype))) or (k_dtype is not None and self._k not in (None, (dim, k_dtype))):
+            raise ValueError(f"norm weights [{dim}] of the rows' type are wanted, queries {q_dtype}, keys {k_dtype}")
 
 
 def _row_strides(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, dim: int, device: torch.device):
@@ -76,10 +76,12 @@ def _check_positions(t: torch.Tensor, rows: int, device: torch.device):
         raise ValueError(f"positions: a contiguous int32 tensor of {rows} on {device} is wanted")
 
 
-def _current(device: torch.device):
-    """Launches go to the current device's current stream: a batch of another device is not served from here."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
+def _stream_of(device: torch.device) -> int:
+    """The current stream, which is the current device's: tensors of another are not served from here."""
+    current = torch.cuda.current_device() if device.type == "cuda" else -1
+    if device.index != current:
         raise ValueError(f"the tensors are on {device}, which is not the current device")
+    return _raw_stream(current) if _raw_stream is not None else int(torch.cuda.current_stream().cuda_stream)
 
 
 _TORCH_DTYPE = {B.PS_F32: torch.float32, B.PS_BF16: torch.bfloat16}
@@ -95,8 +97,7 @@ def rope_rows(geometry: B.ps_geometry, rope: Rope, src: torch.Tensor, positions:
     elif out.shape != src.shape or out.dtype is not dtype or not out.is_contiguous() or out.device != src.device:
         raise ValueError("out: a contiguous tensor like src is wanted")
     rope.check(src.device, geometry.head_dim, dtype, None)
-    _current(src.device)
-    B.ps_rope_rows(geometry, rope.struct, n, src.data_ptr(), row, head, positions.data_ptr(), out.data_ptr(), _stream())
+    B.ps_rope_rows(geometry, rope.struct, n, src.data_ptr(), row, head, positions.data_ptr(), out.data_ptr(), _stream_of(src.device))
     return out
 
 
@@ -142,10 +143,11 @@ class DecodeBatch:
         B.ps_layout_set_visible(self.layout, self.num_requests, prefix_visible)
         self._sync_plan()
 
-    def _stream(self) -> int:
+    def _stream(self, stream: int | None = None) -> int:
         """The current stream, for a launch that reads the tables: behind their upload, whichever stream that went to, and
         they and the workspace live until the launch is done."""
-        stream = _stream()
+        if stream is None:
+            stream = _stream()
         if stream != self._home:
             current = torch.cuda.current_stream()
             # (a launch that is only recorded runs with the graph, whose replays the caller orders)
@@ -186,9 +188,9 @@ class DecodeBatch:
         left alone), keys normed and rotated and values into the cache."""
         rows = self._token_rows(q, k, v, positions)
         rope.check(self.device, self.geometry.head_dim, self.q.dtype if q is not None else None, k.dtype)
-        _current(self.device)
+        stream = self._stream(_stream_of(self.device))
         B.ps_kv_append_rope(self.layout, self.tables.data_ptr(), rope.struct, rows, self.q.data_ptr() if q is not None else 0,
-                            self.kv.data_ptr(), self._sc(), self._stream())
+                            self.kv.data_ptr(), self._sc(), stream)
 
     def _token_rows(self, q, k, v, positions):
         g, n = self.geometry, self.num_requests
@@ -215,9 +217,9 @@ class DecodeBatch:
             raise ValueError("src_k and src_v have the same strides")
         _check_positions(positions, n, self.device)
         rope.check(self.device, d, None, dtype)
-        _current(self.device)
+        stream = self._stream(_stream_of(self.device))
         B.ps_kv_ingest_rope(self.layout, self.tables.data_ptr(), which, rope.struct, src_k.data_ptr(), src_v.data_ptr(), *strides,
-                            positions.data_ptr(), self.kv.data_ptr(), self._sc(), self._stream())
+                            positions.data_ptr(), self.kv.data_ptr(), self._sc(), stream)
 
     def kv_gather(self, which: int, dst_k: torch.Tensor, dst_v: torch.Tensor):
         """The stored segments of one kind back into [T, Hkv, d] tensors, bf16 or float32 (kv_ingest the other way round)."""
@@ -228,9 +230,9 @@ class DecodeBatch:
         strides = _row_strides("dst_k", dst_k, dtype, n, heads, d, self.device)
         if _row_strides("dst_v", dst_v, dtype, n, heads, d, self.device) != strides:
             raise ValueError("dst_k and dst_v have the same strides")
-        _current(self.device)
+        stream = self._stream(_stream_of(self.device))
         B.ps_kv_gather(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(),
-                       B.PS_F32 if dtype is torch.float32 else B.PS_BF16, dst_k.data_ptr(), dst_v.data_ptr(), *strides, self._stream())
+                       B.PS_F32 if dtype is torch.float32 else B.PS_BF16, dst_k.data_ptr(), dst_v.data_ptr(), *strides, stream)
 
     def _segment_tokens(self, which: int) -> int:
         """Tokens that an ingest of one kind of segment takes (adopted blocks aside)."""
@@ -239,9 +241,9 @@ class DecodeBatch:
     def block_summaries(self, which: int, summaries: torch.Tensor, summary_scales: torch.Tensor):
         """Eight-bit bounds of every block's keys: summaries int8 [num_blocks, Hkv, 2, d], summary_scales float32 [num_blocks, Hkv]."""
         self._check_summaries(summaries, summary_scales)
-        _current(self.device)
+        stream = self._stream(_stream_of(self.device))
         B.ps_block_summaries(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(), summaries.data_ptr(),
-                             summary_scales.data_ptr(), self._stream())
+                             summary_scales.data_ptr(), stream)
 
     def _check_summaries(self, summaries, summary_scales):
         heads, n = self.geometry.num_kv_heads, summaries.shape[0]
@@ -317,8 +319,8 @@ class SelectedBatch(DecodeBatch):
         indptr, stride = B.ps_select_lists(self.layout, self.num_requests)
         self._lists = self.tables.view(torch.int32).as_strided((self.geometry.num_kv_heads, int(indptr[-1])), (stride, 1))
 
-    def _stream(self) -> int:
-        stream = super()._stream()
+    def _stream(self, stream: int | None = None) -> int:
+        stream = super()._stream(stream)
         if stream != self._home:
             self.scratch.record_stream(torch.cuda.current_stream())
         return stream
@@ -326,11 +328,11 @@ class SelectedBatch(DecodeBatch):
     def select_blocks(self, summaries: torch.Tensor, summary_scales: torch.Tensor):
         """Scores every block of the shared contexts against the base's queries and writes the lists of the highest."""
         self._check_summaries(summaries, summary_scales)
-        _current(self.device)
-        base = self.base
-        base._stream()                       # (the base's tables, too, behind their upload)
+        base, stream = self.base, _stream_of(self.device)
+        base._stream(stream)                 # (the base's tables, too, behind their upload)
+        self._stream(stream)
         B.ps_select_blocks(base.layout, base.tables.data_ptr(), self.layout, self.tables.data_ptr(), base.q.data_ptr(), summaries.data_ptr(),
-                           summary_scales.data_ptr(), self.scratch.data_ptr(), self._stream())
+                           summary_scales.data_ptr(), self.scratch.data_ptr(), stream)
 
     def follow(self):
         """In line with the base again.  Like the base's append_step it does not wait on the host."""
