@@ -221,15 +221,14 @@ __device__ __forceinline__ uint32_t wave_min_u32(uint32_t x) {
   return uint32_t(__builtin_amdgcn_readlane(int(x), 63));
 }
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) { return ~wave_min_u32(~x); }
-// over 4 or 16 neighbouring lanes
+// over 4, 8 or 16 neighbouring lanes
 template <int N>
 __device__ __forceinline__ uint32_t few_min_u32(uint32_t x) {
   x = min(x, dpp_u32<kXor1>(x, x));
   x = min(x, dpp_u32<kXor2>(x, x));
-  if constexpr (N == 16) {
-    x = min(x, dpp_u32<kHalfMirror>(x, x));
-    x = min(x, dpp_u32<kMirror>(x, x));
-  }
+  static_assert(N == 4 || N == 8 || N == 16, "");
+  if constexpr (N >= 8) x = min(x, dpp_u32<kHalfMirror>(x, x));
+  if constexpr (N == 16) x = min(x, dpp_u32<kMirror>(x, x));
   return uint32_t(__builtin_amdgcn_readfirstlane(int(x)));
 }
 // sum of the lanes up to and with this one
@@ -513,10 +512,15 @@ int32_t launch_select_blocks(const ps_layout* base, const void* dev_tables, cons
 #undef PS_SCORE_C
 #undef PS_SCORE
   const dim3 rows(unsigned(n_choices * g.num_kv_heads));
-  // up to eight keys a thread of a small workgroup; a long context's are shared out over sixteen waves
+  // Four keys a thread and as many waves as that takes; what sixteen waves do not hold so, eight and sixteen a thread; the rest in memory.
+  // Scores and choice, 32 / 768 rows (256 from 4000 on), threads x keys: 875 positions 256x4 8.8 / 16.8 us, 256x8 9.8 / 17.8, 1024x4
+  // 9.3 / 24.8; 1875 positions 512x4 9.1 / 28.3, 256x8 10.3 / 29.0, 1024x4 9.7 / 35.4; 4000 1024x4 9.6 / 21.7, 1024x8 11.1 / 23.0, 512x8
+  // 10.0 / 22.1, 256x16 12.1 / 24.3; 8125 1024x8 13.1 / 23.9 (192 rows), 1024x16 18.1 / 32.6, in memory 18.4 / 31.5; 12500 1024x16 23.6 /
+  // 35.9 (96 rows), in memory 28.4 / 40.5.
 #define PS_CHOOSE(THREADS, PER) hipLaunchKernelGGL((choose_kernel<THREADS, PER>), rows, dim3(THREADS), 0, st, p)
   if (s.most_candidates <= 4 * 256) PS_CHOOSE(256, 4);
-  else if (s.most_candidates <= 8 * 256) PS_CHOOSE(256, 8);
+  else if (s.most_candidates <= 4 * 512) PS_CHOOSE(512, 4);
+  else if (s.most_candidates <= 4 * 1024) PS_CHOOSE(1024, 4);
   else if (s.most_candidates <= 8 * 1024) PS_CHOOSE(1024, 8);
   else if (s.most_candidates <= 16 * 1024) PS_CHOOSE(1024, 16);
   else PS_CHOOSE(1024, 0);
