@@ -62,18 +62,19 @@ class Rope:
             raise ValueError(f"norm weights [{dim}] of the rows' type are wanted, queries {q_dtype}, keys {k_dtype}")
 
 
-def _row_strides(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, dim: int, device: torch.device):
-    """(row, head) strides of rows [rows, heads, dim] with contiguous elements; anything else is refused."""
+def _row_strides(name: str, t: torch.Tensor, dtype: torch.dtype, rows: int, heads: int, dim: int, device: int):
+    """(row, head) strides of rows [rows, heads, dim] with contiguous elements; anything else is refused.  device: its index, -1 = host
+    memory (comparing those takes half as long as comparing torch's device objects, which counts in front of a launch of 3 us)."""
     strides = t.stride()
-    if t.dtype is not dtype or t.shape != (rows, heads, dim) or strides[2] != 1 or t.device != device:
-        raise ValueError(f"{name}: rows [{rows}, {heads}, {dim}] of {dtype} with contiguous elements on {device} are wanted")
+    if t.dtype is not dtype or t.shape != (rows, heads, dim) or strides[2] != 1 or t.get_device() != device or (device < 0 and not t.is_cpu):
+        raise ValueError(f"{name}: rows [{rows}, {heads}, {dim}] of {dtype} with contiguous elements on device {device} are wanted")
     # (of an axis of one the stride is not used, and torch's may be anything)
     return strides[0] if rows > 1 else max(strides[0], dim), strides[1] if heads > 1 else max(strides[1], dim)
 
 
-def _check_positions(t: torch.Tensor, rows: int, device: torch.device):
-    if t.dtype is not torch.int32 or t.shape != (rows,) or (rows > 1 and t.stride(0) != 1) or t.device != device:
-        raise ValueError(f"positions: a contiguous int32 tensor of {rows} on {device} is wanted")
+def _check_positions(t: torch.Tensor, rows: int, device: int):
+    if t.dtype is not torch.int32 or t.shape != (rows,) or not t.is_contiguous() or t.get_device() != device or (device < 0 and not t.is_cpu):
+        raise ValueError(f"positions: a contiguous int32 tensor of {rows} on device {device} is wanted")
 
 
 def _stream_of(device: torch.device) -> int:
@@ -90,8 +91,8 @@ _TORCH_DTYPE = {B.PS_F32: torch.float32, B.PS_BF16: torch.bfloat16}
 def rope_rows(geometry: B.ps_geometry, rope: Rope, src: torch.Tensor, positions: torch.Tensor, out: torch.Tensor | None = None) -> torch.Tensor:
     """Queries of any number of tokens [T, Hq, d] normed and rotated; returns them contiguous (in `out` where given)."""
     dtype, n = _TORCH_DTYPE[geometry.q_dtype], src.shape[0]
-    row, head = _row_strides("src", src, dtype, n, geometry.num_q_heads, geometry.head_dim, src.device)
-    _check_positions(positions, n, src.device)
+    row, head = _row_strides("src", src, dtype, n, geometry.num_q_heads, geometry.head_dim, src.get_device())
+    _check_positions(positions, n, src.get_device())
     if out is None:
         out = torch.empty(src.shape, dtype=dtype, device=src.device)
     elif out.shape != src.shape or out.dtype is not dtype or not out.is_contiguous() or out.device != src.device:
@@ -194,15 +195,15 @@ class DecodeBatch:
 
     def _token_rows(self, q, k, v, positions):
         g, n = self.geometry, self.num_requests
-        heads, d = g.num_kv_heads, g.head_dim
+        heads, d, device = g.num_kv_heads, g.head_dim, self.q.get_device()
         dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
-        strides = _row_strides("k", k, dtype, n, heads, d, self.device)
-        if _row_strides("v", v, dtype, n, heads, d, self.device) != strides:
+        strides = _row_strides("k", k, dtype, n, heads, d, device)
+        if _row_strides("v", v, dtype, n, heads, d, device) != strides:
             raise ValueError("k and v have the same strides")
-        _check_positions(positions, n, self.device)
+        _check_positions(positions, n, device)
         if q is None:
             return B.ps_token_rows(0, k.data_ptr(), v.data_ptr(), 0, 0, *strides, positions.data_ptr())
-        q_strides = _row_strides("q", q, _TORCH_DTYPE[g.q_dtype], n, g.num_q_heads, d, self.device)
+        q_strides = _row_strides("q", q, _TORCH_DTYPE[g.q_dtype], n, g.num_q_heads, d, device)
         if not self.q.is_contiguous():
             raise ValueError("the batch's queries are a contiguous tensor")
         return B.ps_token_rows(q.data_ptr(), k.data_ptr(), v.data_ptr(), *q_strides, *strides, positions.data_ptr())
@@ -210,12 +211,12 @@ class DecodeBatch:
     def kv_ingest_rope(self, which: int, rope: Rope, src_k: torch.Tensor, src_v: torch.Tensor, positions: torch.Tensor):
         """kv_ingest of raw projections [T, Hkv, d]: keys normed and rotated on their way; positions int32 [T]."""
         g, n = self.geometry, self._segment_tokens(which)
-        heads, d = g.num_kv_heads, g.head_dim
+        heads, d, device = g.num_kv_heads, g.head_dim, self.q.get_device()
         dtype = torch.float32 if g.kv_dtype == B.PS_F32 else torch.bfloat16
-        strides = _row_strides("src_k", src_k, dtype, n, heads, d, self.device)
-        if _row_strides("src_v", src_v, dtype, n, heads, d, self.device) != strides:
+        strides = _row_strides("src_k", src_k, dtype, n, heads, d, device)
+        if _row_strides("src_v", src_v, dtype, n, heads, d, device) != strides:
             raise ValueError("src_k and src_v have the same strides")
-        _check_positions(positions, n, self.device)
+        _check_positions(positions, n, device)
         rope.check(self.device, d, None, dtype)
         stream = self._stream(_stream_of(self.device))
         B.ps_kv_ingest_rope(self.layout, self.tables.data_ptr(), which, rope.struct, src_k.data_ptr(), src_v.data_ptr(), *strides,
@@ -224,11 +225,11 @@ class DecodeBatch:
     def kv_gather(self, which: int, dst_k: torch.Tensor, dst_v: torch.Tensor):
         """The stored segments of one kind back into [T, Hkv, d] tensors, bf16 or float32 (kv_ingest the other way round)."""
         g, n, dtype = self.geometry, self._segment_tokens(which), dst_k.dtype
-        heads, d = g.num_kv_heads, g.head_dim
+        heads, d, device = g.num_kv_heads, g.head_dim, self.q.get_device()
         if dtype is not torch.bfloat16 and dtype is not torch.float32:
             raise ValueError("dst_k, dst_v: bf16 or float32 tensors are wanted")
-        strides = _row_strides("dst_k", dst_k, dtype, n, heads, d, self.device)
-        if _row_strides("dst_v", dst_v, dtype, n, heads, d, self.device) != strides:
+        strides = _row_strides("dst_k", dst_k, dtype, n, heads, d, device)
+        if _row_strides("dst_v", dst_v, dtype, n, heads, d, device) != strides:
             raise ValueError("dst_k and dst_v have the same strides")
         stream = self._stream(_stream_of(self.device))
         B.ps_kv_gather(self.layout, self.tables.data_ptr(), which, self.kv.data_ptr(), self._sc(),
