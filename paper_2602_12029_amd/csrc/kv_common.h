@@ -89,7 +89,8 @@ struct KvWriteParams {
 // correction q <- q - (q scale - x) y brings it within one, and by Markstein's theorem (IBM J. Res. Dev. 34, 1990: y correctly
 // rounded, q within one step, the residual exact) the next one to the correctly rounded quotient.  The residual is written with
 // this sign so that -0 keeps its own.  The residuals are exact where they do not underflow: from 2^-10 of the scale on, below
-// which the code is 0 either way, so for any scale from 2^-90; the others, and infinities, are divided.
+// which the code is 0 either way, so for any scale from 2^-90; the others, and infinities, are divided.  Quotients that were checked for the
+// neighbourhood of a rounding boundary instead, and divided there, cost an ingest of 2.2 GB, often ties, 584 us, this 547.
 struct E4m3Encoder {
   float scale, rinv;
   bool divide;   // uniform

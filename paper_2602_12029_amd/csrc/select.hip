@@ -198,8 +198,9 @@ __global__ __launch_bounds__(256) void score_kernel(SelectParams p) {
 //
 // Nothing here is bound but by the chain of its steps: the keys stay in registers, PER a thread (0: in place of the scores, any
 // number), waves meet by DPP rather than through LDS where they can, the members are ranked four at a time, and the block
-// ids are fetched with the scores.  768 rows of up to 1900 positions 12.2 us with keys in LDS and exchanges by ds_bpermute; 32 keys a
-// thread, unrolled in every pass, were bound by fetching their instructions (32 rows of 8188, 34.8 us; sixteen waves to a row 14.2).
+// ids are fetched with the scores.  768 rows of up to 1900 positions 12.2 us with keys in LDS and exchanges by ds_bpermute, 6.8 now; 32 keys a
+// thread, unrolled in every pass, were bound by fetching their instructions (32 rows of 8188, 34.8 us; sixteen waves to a row 14.2, 8.8 with
+// the bins held and the block ids fetched early).
 constexpr int kBins = 256, kFew = 256;
 constexpr uint32_t kTaken = 0xffffffffu;
 

@@ -424,3 +424,36 @@ def test_the_largest_e4m3_tiles(gpu, d, block):
         for h in range(2):
             _check_tile(values[b, h, 0, :m], scales[b, h, 0], ref[i * block:i * block + m, h], mag[i * block:i * block + m, h], "fp8_e4m3", f"{b} {h}")
     case.close()
+
+
+@pytest.mark.parametrize("heads", [8, 3])
+@pytest.mark.parametrize("blocks", [5, 300, 500, 800, 1300])
+def test_however_many_blocks(gpu, heads, blocks):
+    """A block's tiles in one workgroup or shared out over several: bf16 keys as the rows alone come out, e4m3 tiles as by the plain ingest."""
+    from paper_2602_12029_amd import binding as B
+    from paper_2602_12029_amd.runtime import Rope, rope_rows
+    n = 16 * blocks - 7
+    gen = torch.Generator(device="cuda").manual_seed(blocks + heads)
+    k, v = (torch.randn((n, heads, 128), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(2))
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    for dtype in ("bf16", "fp8_e4m3"):
+        w = wl.make_workload("many", wl.Geometry(heads, heads, 128, 16, "bf16", dtype), 1, [n], [[0]], [0], 1.0, seed=1)
+        case = gpu(w)
+        _poison(case)
+        if dtype == "bf16":
+            rope = Rope(500000.0 ** (-np.arange(64) / 64), q_weight=v[0, 0].contiguous(), k_weight=v[0, 0].contiguous())
+            case.batch.kv_ingest_rope(0, rope, k, v, pos)
+            back = torch.empty((2, n, heads, 128), dtype=torch.bfloat16, device="cuda")
+            case.batch.kv_gather(0, back[0], back[1])
+            rows = rope_rows(B.geometry(heads, heads, 128, 16, "bf16", "bf16"), rope, k, pos)
+            torch.cuda.synchronize()
+            assert torch.equal(_bits(back[0]), _bits(rows)) and torch.equal(_bits(back[1]), _bits(v))
+        else:
+            case.batch.kv_ingest_rope(0, Rope([]), k, v, pos)
+            torch.cuda.synchronize()
+            got, scales = case.batch.kv.clone(), case.batch.scales.clone()
+            _poison(case)
+            case.batch.kv_ingest(0, k, v)
+            torch.cuda.synchronize()
+            assert torch.equal(got, case.batch.kv) and torch.equal(_bits(scales), _bits(case.batch.scales))
+        case.close()
