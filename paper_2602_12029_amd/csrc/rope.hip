@@ -283,15 +283,15 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
 
 // ---- ingest: whole segments ------------------------------------------------------------------------------------------------
 // A workgroup takes a pass of a block's tokens (PASS of them; all of an e4m3 block, whose tiles have a scale each) and works
-// through its (head, K|V) tiles, WPT waves to a tile, CH eight-element pieces a lane.  HBM-bound.  The angles of the pass's
+// through its (head, K|V) tiles, WPT of its WAVES waves to a tile, CH eight-element pieces a lane.  HBM-bound.  The angles of the pass's
 // tokens lie in LDS for all heads.  47 thousand tokens of eight heads of 128 in bf16 73 us (387 MB, 5.3 TB/s), 278 thousand into e4m3 tiles
 // 315 (1713 MB, 5.4 TB/s; 440 at the two workgroups a compute unit that the registers gave without a bound, and with quotients
 // that were checked and divided where in doubt).
-template <int D, int KVT, int CH, int WPT>
-__global__ __launch_bounds__(256, CH == 4 && KVT == PS_FP8_E4M3 ? 4 : 2) void ingest_rope_kernel(RopeArgs a, KvWriteParams p, const void* __restrict__ src_k, const void* __restrict__ src_v,
+template <int D, int KVT, int CH, int WPT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, CH == 4 && KVT == PS_FP8_E4M3 ? 4 : 2) void ingest_rope_kernel(RopeArgs a, KvWriteParams p, const void* __restrict__ src_k, const void* __restrict__ src_v,
                                                           int64_t s_tok, int64_t s_head, int entry0, int passes, int tiles_per_team) {
   typedef std::conditional_t<KVT == PS_F32, float, uint16_t> T;
-  constexpr int L = D / 8, kTeams = 4 / WPT, kPass = CH * WPT * 64 / L;   // tokens the teams hold of a tile
+  constexpr int L = D / 8, kTeams = WAVES / WPT, kPass = CH * WPT * 64 / L;   // tokens the teams hold of a tile
   extern __shared__ __attribute__((aligned(16))) float angles[];                                      // [kPass][2][rot / 2]: cosines, sines
   __shared__ float sm_max[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), c8 = lane & (L - 1);
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(256, CH == 4 && KVT == PS_FP8_E4M3 ? 4 : 2) void in
     // a pair a lane, a token a wave
     for (int pair = lane; pair < half; pair += 64) {
       const uint64_t rate = a.turns[pair];
-      for (int t = wave; t < count; t += 4) turn_sincos(turn_of(a.positions[tok0 + t], rate), angles[(2 * t + 1) * half + pair], angles[2 * t * half + pair]);
+      for (int t = wave; t < count; t += WAVES) turn_sincos(turn_of(a.positions[tok0 + t], rate), angles[(2 * t + 1) * half + pair], angles[2 * t * half + pair]);
     }
     __syncthreads();
   }
@@ -442,7 +442,8 @@ int32_t launch_ingest_rope(const ps_layout* lay, const void* dev_tables, int whi
   const int pass_tokens = ch * wpt * 512 / g.head_dim;
   const int64_t passes = (g.block_size + pass_tokens - 1) / pass_tokens;
   const size_t lds = size_t(pass_tokens) * size_t(a.rot) * sizeof(float);
-  const int teams = 4 / wpt, all = (2 * g.num_kv_heads + teams - 1) / teams;   // tiles a team would have alone
+  const int waves = g.num_kv_heads == 1 && wpt == 1 ? 2 : 4;   // (one head has two tiles: 150 thousand float32 tokens 86.6 us with four waves, 65.6 with two)
+  const int teams = waves / wpt, all = (2 * g.num_kv_heads + teams - 1) / teams;   // tiles a team would have alone
   // All tiles of a block in one workgroup, so that its angles are worked out once, where that gives four workgroups a compute
   // unit; a smaller batch has a block's tiles shared out over as many workgroups as that takes (rounded up from a quarter on).  Eight
   // heads, blocks of sixteen 128-wide tokens, one workgroup a block / two / four: 250 blocks bf16 12.6 / 11.3 / 9.0 us, e4m3 13.3 / 10.8 / 8.7;
@@ -456,14 +457,16 @@ int32_t launch_ingest_rope(const ps_layout* lay, const void* dev_tables, int whi
   if (step * passes > INT32_MAX) return PS_ERR_UNSUPPORTED;
   for (int64_t first = 0; first < entries; first += step) {
     const dim3 grid(unsigned(std::min(step, entries - first) * passes), unsigned(slices));
-#define PS_INGEST(D, KVT, CH, WPT)                                                                                           \
-  hipLaunchKernelGGL((ingest_rope_kernel<D, KVT, CH, WPT>), grid, dim3(256), lds, st, a, p, src_k, src_v, s_tok, s_head,      \
+#define PS_INGEST(D, KVT, CH, WPT, WAVES)                                                                                    \
+  hipLaunchKernelGGL((ingest_rope_kernel<D, KVT, CH, WPT, WAVES>), grid, dim3(64 * WAVES), lds, st, a, p, src_k, src_v, s_tok, s_head, \
                      entry0 + int(first), int(passes), per_team)
-#define PS_INGEST_E(D) if (wpt == 4) PS_INGEST(D, PS_FP8_E4M3, 8, 4); else if (ch == 8) PS_INGEST(D, PS_FP8_E4M3, 8, 1); else PS_INGEST(D, PS_FP8_E4M3, 4, 1)
-#define PS_INGEST_T(D) if (e4m3) { PS_INGEST_E(D); } else if (g.kv_dtype == PS_F32) PS_INGEST(D, PS_F32, 4, 1); else PS_INGEST(D, PS_BF16, 4, 1)
+#define PS_INGEST_W(D, KVT, CH) if (waves == 2) PS_INGEST(D, KVT, CH, 1, 2); else PS_INGEST(D, KVT, CH, 1, 4)
+#define PS_INGEST_E(D) if (wpt == 4) PS_INGEST(D, PS_FP8_E4M3, 8, 4, 4); else if (ch == 8) { PS_INGEST_W(D, PS_FP8_E4M3, 8); } else { PS_INGEST_W(D, PS_FP8_E4M3, 4); }
+#define PS_INGEST_T(D) if (e4m3) { PS_INGEST_E(D) } else if (g.kv_dtype == PS_F32) { PS_INGEST_W(D, PS_F32, 4); } else { PS_INGEST_W(D, PS_BF16, 4); }
     if (g.head_dim == 64) { PS_INGEST_T(64); } else if (g.head_dim == 128) { PS_INGEST_T(128); } else { PS_INGEST_T(256); }
 #undef PS_INGEST_T
 #undef PS_INGEST_E
+#undef PS_INGEST_W
 #undef PS_INGEST
   }
   return PS_OK;
