@@ -288,7 +288,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(RopeArgs a, KvWritePar
 // 315 (1713 MB, 5.4 TB/s; 440 at the two workgroups a compute unit that the registers gave without a bound, and with quotients
 // that were checked and divided where in doubt).
 template <int D, int KVT, int CH, int WPT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, CH == 4 && KVT == PS_FP8_E4M3 ? 4 : 2) void ingest_rope_kernel(RopeArgs a, KvWriteParams p, const void* __restrict__ src_k, const void* __restrict__ src_v,
+__global__ __launch_bounds__(64 * WAVES, CH <= 4 && KVT == PS_FP8_E4M3 ? 4 : 2) void ingest_rope_kernel(RopeArgs a, KvWriteParams p, const void* __restrict__ src_k, const void* __restrict__ src_v,
                                                           int64_t s_tok, int64_t s_head, int entry0, int passes, int tiles_per_team) {
   typedef std::conditional_t<KVT == PS_F32, float, uint16_t> T;
   constexpr int L = D / 8, kTeams = WAVES / WPT, kPass = CH * WPT * 64 / L;   // tokens the teams hold of a tile
@@ -436,9 +436,10 @@ int32_t launch_ingest_rope(const ps_layout* lay, const void* dev_tables, int whi
   const KvWriteParams p = make_write_params(lay, dev_tables, kv, scales);
   const bool e4m3 = g.kv_dtype == PS_FP8_E4M3;
   const int64_t pieces = int64_t(g.block_size) * g.head_dim / 8;   // of a tile, eight elements each
-  // (e4m3: 4 or 8 a lane of one wave, 8 a lane of four; else 4 a lane and as many passes as a block has)
+  // (e4m3: 2, 4 or 8 a lane of one wave, 8 a lane of four; else up to 4 a lane and as many passes as a block has.  Blocks of sixteen 64-wide
+  // tokens, 150 thousand of them, with four a lane / two: bf16 one head 36.2 / 23.8 us, two 60.6 / 38.7, eight 127 / 107; e4m3 eight 139 / 97.)
   if (e4m3 && pieces > 2048) return PS_ERR_UNSUPPORTED;
-  const int wpt = e4m3 && pieces > 512 ? 4 : 1, ch = e4m3 && pieces > 256 ? 8 : 4;
+  const int wpt = e4m3 && pieces > 512 ? 4 : 1, ch = e4m3 && pieces > 256 ? 8 : pieces > 128 ? 4 : 2;
   const int pass_tokens = ch * wpt * 512 / g.head_dim;
   const int64_t passes = (g.block_size + pass_tokens - 1) / pass_tokens;
   const size_t lds = size_t(pass_tokens) * size_t(a.rot) * sizeof(float);
@@ -461,11 +462,13 @@ int32_t launch_ingest_rope(const ps_layout* lay, const void* dev_tables, int whi
   hipLaunchKernelGGL((ingest_rope_kernel<D, KVT, CH, WPT, WAVES>), grid, dim3(64 * WAVES), lds, st, a, p, src_k, src_v, s_tok, s_head, \
                      entry0 + int(first), int(passes), per_team)
 #define PS_INGEST_W(D, KVT, CH) if (waves == 2) PS_INGEST(D, KVT, CH, 1, 2); else PS_INGEST(D, KVT, CH, 1, 4)
-#define PS_INGEST_E(D) if (wpt == 4) PS_INGEST(D, PS_FP8_E4M3, 8, 4, 4); else if (ch == 8) { PS_INGEST_W(D, PS_FP8_E4M3, 8); } else { PS_INGEST_W(D, PS_FP8_E4M3, 4); }
-#define PS_INGEST_T(D) if (e4m3) { PS_INGEST_E(D) } else if (g.kv_dtype == PS_F32) { PS_INGEST_W(D, PS_F32, 4); } else { PS_INGEST_W(D, PS_BF16, 4); }
+#define PS_INGEST_C(D, KVT) if (ch == 2) { PS_INGEST_W(D, KVT, 2); } else { PS_INGEST_W(D, KVT, 4); }
+#define PS_INGEST_E(D) if (wpt == 4) PS_INGEST(D, PS_FP8_E4M3, 8, 4, 4); else if (ch == 8) { PS_INGEST_W(D, PS_FP8_E4M3, 8); } else { PS_INGEST_C(D, PS_FP8_E4M3) }
+#define PS_INGEST_T(D) if (e4m3) { PS_INGEST_E(D) } else if (g.kv_dtype == PS_F32) { PS_INGEST_C(D, PS_F32) } else { PS_INGEST_C(D, PS_BF16) }
     if (g.head_dim == 64) { PS_INGEST_T(64); } else if (g.head_dim == 128) { PS_INGEST_T(128); } else { PS_INGEST_T(256); }
 #undef PS_INGEST_T
 #undef PS_INGEST_E
+#undef PS_INGEST_C
 #undef PS_INGEST_W
 #undef PS_INGEST
   }
