@@ -437,9 +437,10 @@ int32_t launch_ingest_rope(const ps_layout* lay, const void* dev_tables, int whi
   const bool e4m3 = g.kv_dtype == PS_FP8_E4M3;
   const int64_t pieces = int64_t(g.block_size) * g.head_dim / 8;   // of a tile, eight elements each
   // (e4m3: 2, 4 or 8 a lane of one wave, 8 a lane of four; else up to 4 a lane and as many passes as a block has.  Blocks of sixteen 64-wide
-  // tokens, 150 thousand of them, with four a lane / two: bf16 one head 36.2 / 23.8 us, two 60.6 / 38.7, eight 127 / 107; e4m3 eight 139 / 97.)
+  // tokens, 150 thousand of them, with four a lane / two: bf16 one head 36.2 / 23.8 us, two 60.6 / 38.7, eight 127 / 107; e4m3 eight 139 / 97.  128-wide ones, 50 thousand, as two passes: one head bf16 17.6 / 14.4, float32 25.8 / 23.5, eight
+  // heads 74.8 / 73.4 and 167.7 / 167.7, twice as many 140.0 / 140.8 and 325.7 / 329.8.)
   if (e4m3 && pieces > 2048) return PS_ERR_UNSUPPORTED;
-  const int wpt = e4m3 && pieces > 512 ? 4 : 1, ch = e4m3 && pieces > 256 ? 8 : pieces > 128 ? 4 : 2;
+  const int wpt = e4m3 && pieces > 512 ? 4 : 1, ch = e4m3 && pieces > 256 ? 8 : pieces > 128 && (e4m3 || g.num_kv_heads > 1) ? 4 : 2;
   const int pass_tokens = ch * wpt * 512 / g.head_dim;
   const int64_t passes = (g.block_size + pass_tokens - 1) / pass_tokens;
   const size_t lds = size_t(pass_tokens) * size_t(a.rot) * sizeof(float);

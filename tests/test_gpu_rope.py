@@ -426,7 +426,7 @@ def test_the_largest_e4m3_tiles(gpu, d, block):
     case.close()
 
 
-@pytest.mark.parametrize("heads", [8, 3])
+@pytest.mark.parametrize("heads", [8, 3, 1])
 @pytest.mark.parametrize("blocks", [5, 300, 500, 800, 1300])
 def test_however_many_blocks(gpu, heads, blocks):
     """A block's tiles in one workgroup or shared out over several: bf16 keys as the rows alone come out, e4m3 tiles as by the plain ingest."""
