@@ -119,7 +119,10 @@ __device__ __forceinline__ void norm8(float (&x)[8], const float (&w)[8], float 
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(x[j], x[j], sum);
-  const float inv = __builtin_amdgcn_rsqf(group_sum<L>(sum) * (1.f / (8 * L)) + eps);
+  const float mean = group_sum<L>(sum) * (1.f / (8 * L)) + eps;
+  float inv = __builtin_amdgcn_rsqf(mean);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(mean < 0x1p-126f) != 0, 0))   // (the instruction takes those for 0; without an eps rows of 1e-19 have them)
+    inv = mean < 0x1p-126f ? __builtin_amdgcn_rsqf(mean * 0x1p48f) * 0x1p24f : inv;
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = (x[j] * inv) * w[j];
 }

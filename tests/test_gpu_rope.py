@@ -457,3 +457,19 @@ def test_however_many_blocks(gpu, heads, blocks):
             torch.cuda.synchronize()
             assert torch.equal(got, case.batch.kv) and torch.equal(_bits(scales), _bits(case.batch.scales))
         case.close()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("bf16", 256)])
+def test_rows_whose_squares_are_subnormal(gpu, dtype, d):
+    """Without an eps, magnitudes of 2^-65 to 2^-64: squares of 2^-130 and more, on a grid of 2^-149, are off by 2^-20 of themselves, as is
+    their mean, its root by half of each: 2^-20, which the few roundings of the rest leave room for in F32."""
+    from paper_2602_12029_amd import binding as B
+    from paper_2602_12029_amd.runtime import Rope, rope_rows
+    rng = np.random.default_rng(d)
+    x = _tensor((rng.choice([-1.0, 1.0], (9, 4, d)) * rng.uniform(1, 2, (9, 4, d)) * 2.0 ** -65).astype(np.float32), dtype)
+    weight = _tensor((1 + 0.3 * rng.standard_normal(d)).astype(np.float32), dtype)
+    got = rope_rows(B.geometry(4, 1, d, 16, dtype, "f32" if dtype == "f32" else "bf16"), Rope([], "halves", weight, None, 0.0), x,
+                    torch.zeros(9, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    ref = orope.norm_rotate(_values(x), np.zeros(9), [], "halves", _values(weight), 0.0)
+    _check(_values(got), ref, np.abs(ref).max(-1, keepdims=True), dtype, f"subnormal squares {dtype} {d}")
